@@ -308,6 +308,111 @@ int cerb_forward_gemm_plan(int32_t product, int32_t M, int32_t N, int32_t K, int
 int cerb_gemm(int32_t dtype, const void* X_dev, const void* W_dev, float* out_dev, int32_t M, int32_t N, int32_t K,
               void* scratch_dev, size_t scratch_bytes, void* stream);
 
+/* ---- Paged-cache operators for a serving loop around these kernels (the paper has no counterpart) ----
+ * Requests come and go, page tables follow them on the GPU, one new token per sequence attends to a cache whose KV heads are
+ * shared by groups of query heads.  Pools as above with H = KV heads: [page][n_kv_heads][16][head_dim].  All calls only enqueue on
+ * `stream`, allocate nothing, keep nothing between calls and return no device-side errors: lengths out of range are taken as the nearest
+ * in range, a page-table entry outside the pool holds no keys, a slot outside the pool is not written.  Calls on one stream follow one another;
+ * calls that may overlap (other streams, graphs replayed side by side) must not share a scratch, nor state that one of them changes.
+ * B, T or rows of 0: nothing to do.  Row and head strides are in elements, multiples of 16 bytes; base addresses 16-byte aligned
+ * (CERB_E_ARG otherwise). */
+
+/* What is known of the requests and the pages that nobody holds. */
+typedef struct cerb_pages {
+  int32_t  B;                   /* requests, <= 8192 */
+  int32_t  max_pages;           /* page-table row stride */
+  int32_t  free_cap;            /* entries that free_pages has room for */
+  int32_t* len;                 /* dev [B] tokens held */
+  int32_t* page_table;          /* dev [B][max_pages]; a request holds the first ceil(len / 16) entries */
+  int32_t* free_pages;          /* dev [free_cap]: a stack of pages, the top at n_free - 1 */
+  int32_t* n_free;              /* dev [1] */
+} cerb_pages;
+
+/* Room for the tokens of a step.  Request b wants n_new[b] tokens (dev [B]; negative = 0) behind its len[b], in the rows row_off[b] ..
+ * of the step's buffers (row_off dev [B+1]: the exclusive sums of n_new).  In the order of the requests: a request gets its tokens, and the
+ * new pages they need from the top of the stack on, if they fit its table row and end within `rows` rows and the pages wanted up to and
+ * including it (by requests that fit) are there; a request that needs no new page needs no page to be there.  Otherwise it gets none.
+ * granted dev [B]: n_new or 0.  len and n_free change accordingly.  slot, pos, seq dev [rows]: of row r of a granted request its physical slot
+ * (page * 16 + row of the page), its position (len + r - row_off[b]) and the request; -1 for other rows and behind the last one.
+ * CERB_E_SHAPE: more than 8192 requests, B * max_pages of 2^31 or more, more than 2^30 rows. */
+int cerb_pages_plan(const cerb_pages* state, const int32_t* n_new, int32_t rows, int32_t* slot, int32_t* pos, int32_t* seq,
+                    int32_t* row_off, int32_t* granted, void* stream);
+
+/* Cuts every request down to keep[b] tokens (dev [B]; more than it has = it stays as it is; 0 = it is done) and gives back the pages that
+ * it then does not need; their table entries become -1.  The last page of the last request is given back first, so that a trim to
+ * the lengths before a plan restores the stack.  Pages that the stack has no room for are dropped. */
+int cerb_pages_trim(const cerb_pages* state, const int32_t* keep, void* stream);
+
+/* Writes a step's keys and values into their slots.  With k_min and k_max (both or neither), element-wise minimum and maximum of the keys of a
+ * page: of those of this call, and of what is there unless this call writes the page's slot 0 (which begins a page anew; NaN if a key is).
+ * A page's tokens must be next to one another in the list, as cerb_pages_plan leaves them, and no slot come twice; otherwise what the pages
+ * concerned hold is undefined. */
+typedef struct cerb_kv_append_args {
+  int32_t dtype;                /* CERB_BF16 | CERB_F32 */
+  int32_t T, n_kv_heads, head_dim;              /* head_dim 64 or 128 */
+  const void *k, *v;            /* dev [T][n_kv_heads][head_dim], strided */
+  int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  const int32_t* slot;          /* dev [T]; negative = not written */
+  void *k_pool, *v_pool;        /* dev [pages][n_kv_heads][16][head_dim] */
+  void *k_min, *k_max;          /* dev [pages][n_kv_heads][head_dim], or NULL */
+  int32_t n_pool_pages;
+} cerb_kv_append_args;
+int cerb_kv_append(const cerb_kv_append_args* args, void* stream);
+
+/* Attention of one new token per sequence (its own key is in the cache: slot len - 1):
+ * out[b][h] = softmax over s of scale * q[b][h] . k[s], times v[s], with the KV head h / (n_heads / n_kv_heads); s are the
+ * slots max(0, len[b] - window) .. len[b] - 1 (window 0: all), with a list those of them in the pages that it names: sel[b][kv head][i], i < n_sel[b],
+ * logical pages in any order, entries outside the sequence count nothing, a page that comes twice counts twice.  No slots: out 0, lse -infinity.
+ * lse = natural log of the softmax denominator.  Any n_heads divisible by n_kv_heads. */
+typedef struct cerb_paged_attn_args {
+  int32_t dtype;                /* CERB_BF16 | CERB_F32 */
+  int32_t B, n_heads, n_kv_heads, head_dim;     /* head_dim 64 or 128 */
+  int32_t max_pages, n_pool_pages;
+  const void* q;                /* dev [B][n_heads][head_dim], strided */
+  int64_t q_row_stride, q_head_stride;
+  const void *k_pool, *v_pool;
+  const int32_t* page_table;    /* dev [B][max_pages] */
+  const int32_t* len;           /* dev [B] */
+  const int32_t *sel, *n_sel;   /* dev [B][n_kv_heads][max_sel], [B]; or both NULL */
+  int32_t max_sel;
+  void* out;                    /* dev [B][n_heads][head_dim] */
+  float* lse;                   /* dev [B][n_heads] or NULL */
+  float scale;
+  int32_t max_len;              /* the longest length to expect: sizes the launch; longer ones are right but slower */
+  int32_t window;
+  void* scratch;                /* dev, cerb_paged_attention_scratch_bytes() for the same numbers; need not be initialised */
+  size_t scratch_bytes;
+} cerb_paged_attn_args;
+/* max_sel 0: no list */
+int cerb_paged_attention_scratch_bytes(int32_t dtype, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_len,
+                                       int32_t window, int32_t max_sel, size_t* bytes_out);
+int cerb_paged_attention(const cerb_paged_attn_args* args, void* stream);
+
+/* Picks the pages that a new token's queries may attend to most, per sequence and KV head.  A page's score is the largest, over the query heads of the KV head,
+ * of sum_d max(q_d * k_min_d, q_d * k_max_d): no key of the page has a larger q . k.  The first n_first and the last n_last pages are always taken (n_first +
+ * n_last <= max_sel), then the best scores, until max_sel are; all of a sequence of max_sel pages or fewer.  Decisions are made in
+ * exact arithmetic, up to the rounding of sums of fp64; equal scores: the lower page; a score that is not a number is above all others.
+ * sel: logical pages in ascending order, -1 behind the last one; n_sel[b] = min(pages of b, max_sel).
+ * CERB_E_SHAPE: max_pages above 131072 (2 097 152 tokens), more than 64 query heads to a KV head, B * n_kv_heads of 2^23 or more. */
+typedef struct cerb_page_select_args {
+  int32_t dtype;                /* CERB_BF16 | CERB_F32 */
+  int32_t B, n_heads, n_kv_heads, head_dim;     /* head_dim 64 or 128 */
+  int32_t max_pages, n_pool_pages;
+  const void* q;                /* dev [B][n_heads][head_dim], strided */
+  int64_t q_row_stride, q_head_stride;
+  const void *k_min, *k_max;    /* dev [pages][n_kv_heads][head_dim] */
+  const int32_t* page_table;    /* dev [B][max_pages] */
+  const int32_t* len;           /* dev [B] */
+  int32_t max_sel, n_first, n_last;
+  int32_t max_len;              /* the longest length to expect: sizes the launch; longer ones are right but slower */
+  int32_t *sel, *n_sel;         /* dev [B][n_kv_heads][max_sel], [B] */
+  void* scratch;                /* dev, cerb_page_select_scratch_bytes(); need not be initialised */
+  size_t scratch_bytes;
+} cerb_page_select_args;
+int cerb_page_select_scratch_bytes(int32_t dtype, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_pages,
+                                   int32_t max_len, size_t* bytes_out);
+int cerb_page_select(const cerb_page_select_args* args, void* stream);
+
 /* Synchronous read-back of the per-sequence state (any pointer may be NULL):
  * len_host [B], root_host [B], h_last_host [B][d_model] in the model dtype. */
 int cerb_read_state(cerb_ctx* ctx, int32_t* len_host, int32_t* root_host, void* h_last_host, void* stream);

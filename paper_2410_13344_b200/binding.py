@@ -33,6 +33,8 @@ EXPORTS = [
     "cerb_read_state", "cerb_device_status", "cerb_launch_count", "cerb_strerror", "cerb_profile_enable",
     "cerb_profile_read", "cerb_tree_attention_noalloc", "cerb_set_wait_cycles", "cerb_wait_diagnosis", "cerb_tree_attention_noalloc_status", "cerb_launch_order_table", "cerb_last_forward_rows",
     "cerb_gemm_plan", "cerb_forward_gemm_plan",
+    "cerb_pages_plan", "cerb_pages_trim", "cerb_kv_append", "cerb_paged_attention_scratch_bytes", "cerb_paged_attention",
+    "cerb_page_select_scratch_bytes", "cerb_page_select",
 ]
 
 
@@ -82,6 +84,44 @@ class AttnArgs(C.Structure):
     ]
 
 
+class Pages(C.Structure):
+    _fields_ = [
+        ("B", C.c_int32), ("max_pages", C.c_int32), ("free_cap", C.c_int32),
+        ("len", C.c_void_p), ("page_table", C.c_void_p), ("free_pages", C.c_void_p), ("n_free", C.c_void_p),
+    ]
+
+
+class KvAppendArgs(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int32), ("T", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("k", C.c_void_p), ("v", C.c_void_p),
+        ("k_row_stride", C.c_int64), ("k_head_stride", C.c_int64), ("v_row_stride", C.c_int64), ("v_head_stride", C.c_int64),
+        ("slot", C.c_void_p), ("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("k_min", C.c_void_p), ("k_max", C.c_void_p),
+        ("n_pool_pages", C.c_int32),
+    ]
+
+
+class PagedAttnArgs(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int32), ("B", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("max_pages", C.c_int32), ("n_pool_pages", C.c_int32),
+        ("q", C.c_void_p), ("q_row_stride", C.c_int64), ("q_head_stride", C.c_int64), ("k_pool", C.c_void_p), ("v_pool", C.c_void_p),
+        ("page_table", C.c_void_p), ("len", C.c_void_p), ("sel", C.c_void_p), ("n_sel", C.c_void_p), ("max_sel", C.c_int32),
+        ("out", C.c_void_p), ("lse", C.c_void_p), ("scale", C.c_float), ("max_len", C.c_int32), ("window", C.c_int32),
+        ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t),
+    ]
+
+
+class PageSelectArgs(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int32), ("B", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("max_pages", C.c_int32), ("n_pool_pages", C.c_int32),
+        ("q", C.c_void_p), ("q_row_stride", C.c_int64), ("q_head_stride", C.c_int64), ("k_min", C.c_void_p), ("k_max", C.c_void_p),
+        ("page_table", C.c_void_p), ("len", C.c_void_p), ("max_sel", C.c_int32), ("n_first", C.c_int32), ("n_last", C.c_int32),
+        ("max_len", C.c_int32), ("sel", C.c_void_p), ("n_sel", C.c_void_p), ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t),
+    ]
+
+
 _lib = None
 
 
@@ -116,6 +156,13 @@ def lib():
         L.cerb_gemm_scratch_bytes.argtypes = [C.c_int32] * 3 + [C.POINTER(C.c_size_t)]
         L.cerb_gemm.argtypes = [C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
                                 C.c_void_p, C.c_size_t, C.c_void_p]
+        L.cerb_pages_plan.argtypes = [C.POINTER(Pages), C.c_void_p, C.c_int32] + [C.c_void_p] * 6
+        L.cerb_pages_trim.argtypes = [C.POINTER(Pages), C.c_void_p, C.c_void_p]
+        L.cerb_kv_append.argtypes = [C.POINTER(KvAppendArgs), C.c_void_p]
+        L.cerb_paged_attention_scratch_bytes.argtypes = [C.c_int32] * 8 + [C.POINTER(C.c_size_t)]
+        L.cerb_paged_attention.argtypes = [C.POINTER(PagedAttnArgs), C.c_void_p]
+        L.cerb_page_select_scratch_bytes.argtypes = [C.c_int32] * 7 + [C.POINTER(C.c_size_t)]
+        L.cerb_page_select.argtypes = [C.POINTER(PageSelectArgs), C.c_void_p]
         L.cerb_gemm_plan.argtypes = [C.c_int32] * 4 + [C.c_void_p]
         L.cerb_read_state.argtypes = [C.c_void_p] * 5
         L.cerb_device_status.argtypes = [C.c_void_p, C.c_void_p]
@@ -484,3 +531,192 @@ def gemm(X: torch.Tensor, W: torch.Tensor, scratch: Optional[torch.Tensor] = Non
     sp = (scratch.data_ptr() + 255) // 256 * 256
     _check(lib().cerb_gemm(dt, X.data_ptr(), W.data_ptr(), out.data_ptr(), M, N, K, sp, scratch.numel() - 256, _stream()), "cerb_gemm")
     return out
+
+
+# ---- paged-cache operators of a serving loop (see the section on them in cerb.h)
+
+
+def _refuse(code: int, what: str, why: str):
+    e = CerbError(code, what)
+    e.args = ("%s: %s" % (e.args[0], why),)
+    raise e
+
+
+def _need(ok: bool, what: str, why: str):
+    if not ok:
+        _refuse(E_ARG, what, why)
+
+
+def _on_device(what: str, device: torch.device, *tensors):
+    """All of them in that GPU's memory, whole numbers (dtype int32) in one piece."""
+    _need(device.type == "cuda", what, "tensors must be on a GPU")
+    for t in tensors:
+        _need(t.device == device, what, "tensors are on different devices")
+        _need(t.dtype == torch.int32 and t.is_contiguous(), what, "lengths, tables, lists and counts are contiguous int32 tensors")
+
+
+def _call(fn, what: str, device: torch.device, *args):
+    """On the tensors' own device, and the stream that is current there."""
+    if device.index == torch.cuda.current_device():
+        rc = fn(*args, _stream())
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, _stream())
+    _check(rc, what)
+
+
+class PagePlan(NamedTuple):
+    slot: torch.Tensor           # [rows] physical slots, -1 where a row is nobody's
+    pos: torch.Tensor            # [rows] positions
+    seq: torch.Tensor            # [rows] requests
+    row_off: torch.Tensor        # [B + 1] first row of every request
+    granted: torch.Tensor        # [B] tokens that a request got room for: all it wanted, or 0
+
+
+def _pages(what: str, n: torch.Tensor, lens, page_table, free_pages, n_free) -> Pages:
+    _on_device(what, lens.device, n, lens, page_table, free_pages, n_free)
+    B = lens.numel()
+    _need(lens.dim() == 1 and n.shape == lens.shape and page_table.dim() == 2 and page_table.shape[0] == B and free_pages.dim() == 1
+          and n_free.numel() == 1, what, "lens [B], one number a request, page_table [B][max_pages], free_pages [capacity], n_free [1]")
+    _need(page_table.shape[1] >= 1, what, "a table has one column at least")
+    return Pages(B, page_table.shape[1], free_pages.numel(), lens.data_ptr(), page_table.data_ptr(), free_pages.data_ptr(), n_free.data_ptr())
+
+
+def pages_plan(n_new: torch.Tensor, lens: torch.Tensor, page_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor,
+               rows: int) -> PagePlan:
+    """Room for n_new[b] more tokens of every request, in place: lens, page_table, free_pages and n_free are the state of the cache
+    (see cerb_pages_plan); `rows` rows of a step's buffers describe the new tokens."""
+    _need(rows >= 0, "cerb_pages_plan", "rows is negative")
+    a = _pages("cerb_pages_plan", n_new, lens, page_table, free_pages, n_free)
+    if a.B > 8192 or rows > 1 << 30:                         # (ahead of the allocation)
+        _refuse(E_SHAPE, "cerb_pages_plan", "more than 8192 requests or 2^30 rows")
+    pad = (rows + 3) // 4 * 4
+    out = torch.empty(3 * pad + 2 * a.B + 1, dtype=torch.int32, device=lens.device)
+    at = out.data_ptr()
+    p = PagePlan(out[:rows], out[pad:pad + rows], out[2 * pad:2 * pad + rows], out[3 * pad:3 * pad + a.B + 1], out[3 * pad + a.B + 1:])
+    _call(lib().cerb_pages_plan, "cerb_pages_plan", lens.device, C.byref(a), n_new.data_ptr(), rows, at, at + 4 * pad, at + 8 * pad, at + 12 * pad,
+          at + 12 * pad + 4 * (a.B + 1))
+    return p
+
+
+def pages_trim(keep: torch.Tensor, lens: torch.Tensor, page_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor) -> None:
+    """Cuts every request down to keep[b] tokens and gives its other pages back, in place (see cerb_pages_trim)."""
+    a = _pages("cerb_pages_trim", keep, lens, page_table, free_pages, n_free)
+    _call(lib().cerb_pages_trim, "cerb_pages_trim", lens.device, C.byref(a), keep.data_ptr())
+
+
+_DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _rows(what: str, name: str, t: torch.Tensor, heads: int, head_dim: int):
+    """(row stride, head stride) of a [rows][heads][head_dim] operand."""
+    _need(t.dim() == 3 and t.shape[1] == heads and t.shape[2] == head_dim and t.stride(2) == 1, what,
+          "%s is [rows][%d][%d], the elements of a head next to one another" % (name, heads, head_dim))
+    return t.stride(0), t.stride(1)
+
+
+def _pools(what: str, *pools) -> tuple:
+    """(pages, KV heads, head_dim, dtype code) of pools [pages][KV heads][16][head_dim]."""
+    k = pools[0]
+    _need(k.dim() == 4 and k.shape[2] == PAGE, what, "pools are [pages][KV heads][16][head_dim]")
+    for t in pools:
+        _need(t.shape == k.shape and t.dtype == k.dtype and t.device == k.device and t.is_contiguous(), what, "the pools are alike and contiguous")
+    _need(k.dtype in _DTYPES, what, "bfloat16 or float32")
+    return k.shape[0], k.shape[1], k.shape[3], _DTYPES[k.dtype]
+
+
+def _summaries(what: str, k_min, k_max, dtype, device):
+    _need(k_min.dim() == 3 and k_min.shape == k_max.shape and k_min.is_contiguous() and k_max.is_contiguous(), what,
+          "k_min and k_max are [pages][KV heads][head_dim]")
+    _need(k_min.dtype == dtype and k_max.dtype == dtype and k_min.device == device and k_max.device == device, what,
+          "k_min and k_max have another type or device")
+
+
+def kv_append(k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor,
+              k_min: Optional[torch.Tensor] = None, k_max: Optional[torch.Tensor] = None) -> None:
+    """Writes k and v [T][KV heads][head_dim] (views into a packed product will do) into their slots of the pools, and keeps the pages' minima and
+    maxima (see cerb_kv_append)."""
+    what = "cerb_kv_append"
+    n_pages, Hk, D, dt = _pools(what, k_pool, v_pool)
+    _on_device(what, k_pool.device, slot)
+    T = slot.numel()
+    kr, kh = _rows(what, "k", k, Hk, D)
+    vr, vh = _rows(what, "v", v, Hk, D)
+    _need(k.shape[0] == T and v.shape[0] == T, what, "a slot for every row")
+    _need(k.dtype == v.dtype == k_pool.dtype and k.device == v.device == k_pool.device, what, "k, v and the pools differ in type or device")
+    _need((k_min is None) == (k_max is None), what, "k_min and k_max come together")
+    if k_min is not None:
+        _summaries(what, k_min, k_max, k_pool.dtype, k_pool.device)
+        _need(k_min.shape == (n_pages, Hk, D), what, "k_min and k_max are of other pages than the pools")
+    a = KvAppendArgs(dt, T, Hk, D, k.data_ptr(), v.data_ptr(), kr, kh, vr, vh, slot.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), _ptr(k_min),
+                     _ptr(k_max), n_pages)
+    _call(lib().cerb_kv_append, what, k_pool.device, C.byref(a))
+
+
+def _queries(what: str, q, Hk: int, D: int, dtype, device, page_table, lens):
+    _need(q.dim() == 3 and q.shape[1] >= 1 and Hk >= 1 and q.shape[1] % Hk == 0, what, "q is [B][heads][head_dim], its heads a multiple of the KV heads")
+    _need(q.dtype == dtype and q.device == device, what, "q and the cache differ in type or device")
+    _on_device(what, device, page_table, lens)
+    B = q.shape[0]
+    _need(lens.shape == (B,) and page_table.dim() == 2 and page_table.shape[0] == B and page_table.shape[1] >= 1, what,
+          "a length and a row of the page table for every sequence")
+    return _rows(what, "q", q, q.shape[1], D)
+
+
+def _scratch(what: str, given: Optional[torch.Tensor], need: int, device) -> Optional[torch.Tensor]:
+    if given is None:
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _need(given.device == device and given.is_contiguous() and given.dtype == torch.uint8, what, "scratch is a contiguous uint8 tensor on the same device")
+    return given
+
+
+def page_select(q: torch.Tensor, k_min: torch.Tensor, k_max: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor, n_pages: int, max_len: int,
+                n_first: int = 1, n_last: int = 1, scratch: Optional[torch.Tensor] = None):
+    """The n_pages pages of every (sequence, KV head) that hold the largest upper bounds of q . k, the first n_first and the last n_last always among
+    them (see cerb_page_select).  Returns (sel [B][KV heads][n_pages] ascending and -1 behind, n_sel [B])."""
+    what = "cerb_page_select"
+    _need(k_min.dtype in _DTYPES, what, "bfloat16 or float32")
+    _summaries(what, k_min, k_max, k_min.dtype, k_min.device)
+    P, Hk, D = k_min.shape
+    qr, qh = _queries(what, q, Hk, D, k_min.dtype, k_min.device, page_table, lens)
+    _need(n_pages >= 1 and n_first >= 0 and n_last >= 0 and max_len >= 1, what, "counts are not negative, n_pages and max_len one at least")
+    B, H, _ = q.shape
+    dt, mp = _DTYPES[q.dtype], page_table.shape[1]
+    nb = C.c_size_t(0)
+    _check(lib().cerb_page_select_scratch_bytes(dt, B, H, Hk, D, mp, max_len, C.byref(nb)), what)
+    scratch = _scratch(what, scratch, nb.value, q.device)
+    sel = torch.empty(B, Hk, n_pages, dtype=torch.int32, device=q.device)
+    n_sel = torch.empty(B, dtype=torch.int32, device=q.device)
+    a = PageSelectArgs(dt, B, H, Hk, D, mp, P, q.data_ptr(), qr, qh, k_min.data_ptr(), k_max.data_ptr(), page_table.data_ptr(), lens.data_ptr(), n_pages,
+                       n_first, n_last, max_len, sel.data_ptr(), n_sel.data_ptr(), _ptr(scratch), 0 if scratch is None else scratch.numel())
+    _call(lib().cerb_page_select, what, q.device, C.byref(a))
+    return sel, n_sel
+
+
+def paged_attention(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor, scale: float,
+                    max_len: int, window: int = 0, sel: Optional[torch.Tensor] = None, n_sel: Optional[torch.Tensor] = None, want_lse: bool = True,
+                    scratch: Optional[torch.Tensor] = None):
+    """Attention of one new token per sequence, q [B][heads][head_dim] (a view into a packed product will do), over the paged cache, over its last
+    `window` tokens, or over the pages of page_select's lists (see cerb_paged_attention).  Returns (out, lse)."""
+    what = "cerb_paged_attention"
+    n_pages, Hk, D, dt = _pools(what, k_pool, v_pool)
+    qr, qh = _queries(what, q, Hk, D, k_pool.dtype, k_pool.device, page_table, lens)
+    _need(max_len >= 1 and window >= 0, what, "max_len is one at least, window not negative")
+    B, H, _ = q.shape
+    _need((sel is None) == (n_sel is None), what, "sel and n_sel come together")
+    max_sel = 0
+    if sel is not None:
+        _on_device(what, q.device, sel, n_sel)
+        _need(sel.dim() == 3 and sel.shape[0] == B and sel.shape[1] == Hk and sel.shape[2] >= 1 and n_sel.shape == (B,), what,
+              "sel is [B][KV heads][pages], n_sel [B]")
+        max_sel = sel.shape[2]
+    nb = C.c_size_t(0)
+    _check(lib().cerb_paged_attention_scratch_bytes(dt, B, H, Hk, D, max_len, window, max_sel, C.byref(nb)), what)
+    scratch = _scratch(what, scratch, nb.value, q.device)
+    out = torch.empty(B, H, D, dtype=q.dtype, device=q.device)
+    lse = torch.empty(B, H, dtype=torch.float32, device=q.device) if want_lse else None
+    a = PagedAttnArgs(dt, B, H, Hk, D, page_table.shape[1], n_pages, q.data_ptr(), qr, qh, k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(),
+                      lens.data_ptr(), _ptr(sel), _ptr(n_sel), max_sel, out.data_ptr(), _ptr(lse), scale, max_len, window, _ptr(scratch),
+                      0 if scratch is None else scratch.numel())
+    _call(lib().cerb_paged_attention, what, q.device, C.byref(a))
+    return out, lse

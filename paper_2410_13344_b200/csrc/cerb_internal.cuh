@@ -105,6 +105,18 @@ inline cudaError_t launch_pdl_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
+// Lets a kernel have `bytes` of dynamic shared memory on the current device, once per device (`done`: a bit for each of the first 64).
+template <typename K>
+inline int allow_smem(K kern, std::atomic<uint64_t>& done, int bytes) {
+  int dev = 0;
+  CERB_CUDA_OK(cudaGetDevice(&dev));
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (done & bit) return CERB_OK;
+  CERB_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  done |= bit;
+  return CERB_OK;
+}
+
 constexpr int kPathMax = CERB_MAX_DEPTH + 1;
 // Rows of one prefill forward.  A forward streams all the weights whatever its row count, so short chunks pay for the
 // stream again and again: a 2048-token prompt of the 7B shape took 73.7 ms in 128-token chunks (16 weight streams,

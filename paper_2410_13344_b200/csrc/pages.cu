@@ -1,0 +1,395 @@
+// Bookkeeping of a paged KV cache, and the append into it.
+#include <string.h>
+
+#include "cerb_internal.cuh"
+
+namespace cerb {
+
+namespace {
+
+constexpr int PLAN_THREADS = 1024;
+constexpr int PLAN_CLUSTER = 8;
+// Up to this many rows one CTA fills them; more are spread over a cluster.
+constexpr int kPlanRowsOneCta = 8192;
+constexpr int kMaxRequests = 8192;      // four words each of a CTA's shared memory
+
+struct PagesParams {
+  int32_t *len, *page_table, *free_pages, *n_free;
+  const int32_t* n_new;                 // plan: tokens that each request wants; trim: the lengths to keep
+  int32_t *slot, *pos, *seq, *row_off, *granted;
+  int B, max_pages, free_cap, rows;
+};
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
+__device__ __forceinline__ int pages_of(int tokens) { return (int)(((unsigned)tokens + CERB_PAGE - 1) / CERB_PAGE); }
+
+// Inclusive sum over the CTA's threads; `total` is that of all.
+template <typename T>
+__device__ __forceinline__ T block_scan(T v, T* red, T& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const T u = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += u;
+  }
+  if (lane == 31) red[warp] = v;
+  __syncthreads();
+  T w = red[lane];
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const T u = __shfl_up_sync(0xffffffffu, w, o);
+    if (lane >= o) w += u;
+  }
+  total = __shfl_sync(0xffffffffu, w, 31);
+  const T before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
+  __syncthreads();
+  return v + (warp ? before : 0);
+}
+
+// The lengths of a request as the kernels use them: what is out of range is taken to the nearest that is in range.
+__device__ __forceinline__ int held_tokens(const PagesParams& p, int b) { return min(max(p.len[b], 0), p.max_pages * CERB_PAGE); }
+
+// The last request that begins at or before item i; ends[b]: first item behind request b.
+__device__ __forceinline__ int find_request(const int* ends, int B, int i) {
+  int lo = 0, hi = B - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (ends[mid] <= i) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Two prefix sums over the requests (rows, and pages of those that fit) and then a row per element: its request, position and slot.
+// A launch and nothing else: every CTA of the cluster sums up for itself, and lengths and free count change behind the cluster's
+// barrier, when all have read them.  New pages never lie where a row of this call finds an old one, so the table may change before.
+template <bool CLUSTER>
+__global__ void __launch_bounds__(PLAN_THREADS, 1) pages_plan_kernel(const PagesParams p) {
+  extern __shared__ __align__(16) int sm[];
+  int *ends = sm, *lens = ends + p.B, *base = lens + p.B, *give = base + p.B;     // rows before and of b, length, new pages before, 1 if granted
+  __shared__ long long red_rows[32];
+  __shared__ int red_pages[32];
+  const int tid = threadIdx.x;
+  const unsigned cta = CLUSTER ? blockIdx.x : 0, ctas = CLUSTER ? PLAN_CLUSTER : 1;
+  griddep_wait();
+  griddep_launch();
+  const int n_free = min(max(*p.n_free, 0), p.free_cap);
+  long long rows_before = 0;
+  int pages_before = 0, taken = 0;
+  for (int b0 = 0; b0 < p.B; b0 += PLAN_THREADS) {
+    const int b = b0 + tid;
+    const bool live = b < p.B;
+    const int len = live ? held_tokens(p, b) : 0, n = live ? max(p.n_new[b], 0) : 0;
+    long long rows_total;
+    const long long end = rows_before + block_scan((long long)n, red_rows, rows_total);
+    const bool fits = live && (long long)len + n <= (long long)p.max_pages * CERB_PAGE && end <= p.rows;
+    const int need = fits ? pages_of(len + n) - pages_of(len) : 0;
+    int pages_total;
+    const int cum = pages_before + block_scan(need, red_pages, pages_total);
+    const bool ok = fits && (need == 0 || cum <= n_free);
+    if (live) {
+      ends[b] = (int)min(end, 0x7fffffffll);
+      lens[b] = len;
+      base[b] = cum - need;
+      give[b] = ok;
+      if (cta == 0) {
+        p.granted[b] = ok ? n : 0;
+        p.row_off[b + 1] = (int)min(end, 0x7fffffffll);
+      }
+    }
+    // (the ones with new pages that get them are the first ones)
+    int t;
+    block_scan(ok ? need : 0, red_pages, t);
+    taken += t;
+    rows_before += rows_total;
+    pages_before += pages_total;
+  }
+  if (cta == 0 && tid == 0) p.row_off[0] = 0;
+  if (CLUSTER) cluster_arrive();
+  __syncthreads();
+  const int total = (int)min(rows_before, (long long)p.rows);
+  const bool wide = !(((uintptr_t)p.slot | (uintptr_t)p.pos | (uintptr_t)p.seq) & 15);
+  for (int r0 = 4 * (int)(cta * PLAN_THREADS + tid); r0 < p.rows; r0 += 4 * (int)(ctas * PLAN_THREADS)) {
+    int slot[4], pos[4], seq[4];
+    int b = r0 < total ? find_request(ends, p.B, r0) : 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = r0 + i;
+      slot[i] = pos[i] = seq[i] = -1;
+      if (r >= total) continue;
+      while (ends[b] <= r) ++b;
+      if (!give[b]) continue;
+      const int first = b ? ends[b - 1] : 0, len = lens[b], at = len + r - first, j = at / CERB_PAGE, held = pages_of(len);
+      int32_t* entry = p.page_table + (size_t)b * p.max_pages + j;
+      int page;
+      if (j < held) {
+        page = *entry;
+      } else {
+        page = p.free_pages[n_free - 1 - base[b] - (j - held)];
+        if (at % CERB_PAGE == 0) *entry = page;
+      }
+      slot[i] = page * CERB_PAGE + at % CERB_PAGE;
+      pos[i] = at;
+      seq[i] = b;
+    }
+    if (wide && r0 + 3 < p.rows) {
+      *reinterpret_cast<int4*>(p.slot + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+      *reinterpret_cast<int4*>(p.pos + r0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+      *reinterpret_cast<int4*>(p.seq + r0) = make_int4(seq[0], seq[1], seq[2], seq[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (r0 + i < p.rows) { p.slot[r0 + i] = slot[i]; p.pos[r0 + i] = pos[i]; p.seq[r0 + i] = seq[i]; }
+    }
+  }
+  if (CLUSTER) cluster_wait();
+  if (cta != 0) return;
+  for (int b = tid; b < p.B; b += PLAN_THREADS)
+    if (give[b]) p.len[b] = lens[b] + ends[b] - (b ? ends[b - 1] : 0);
+  if (tid == 0) *p.n_free = n_free - taken;
+}
+
+// Pages behind the lengths to keep go back to the list, the last one of the last request first: a trim to the lengths before a
+// plan leaves the list as it was.
+__global__ void __launch_bounds__(PLAN_THREADS, 1) pages_trim_kernel(const PagesParams p) {
+  extern __shared__ __align__(16) int sm[];
+  int *ends = sm, *news = ends + p.B;                          // pages given back before and of b; the length kept
+  __shared__ int red_pages[32];
+  const int tid = threadIdx.x;
+  const unsigned cta = blockIdx.x;
+  griddep_wait();
+  griddep_launch();
+  const int n_free = min(max(*p.n_free, 0), p.free_cap);
+  int total = 0;
+  for (int b0 = 0; b0 < p.B; b0 += PLAN_THREADS) {
+    const int b = b0 + tid;
+    const int len = b < p.B ? held_tokens(p, b) : 0, keep = b < p.B ? min(max(p.n_new[b], 0), len) : 0;
+    int t;
+    const int end = total + block_scan(pages_of(len) - pages_of(keep), red_pages, t);
+    if (b < p.B) { ends[b] = end; news[b] = keep; }
+    total += t;
+  }
+  cluster_arrive();
+  __syncthreads();
+  for (int i = (int)(cta * PLAN_THREADS + tid); i < total; i += PLAN_CLUSTER * PLAN_THREADS) {
+    const int b = find_request(ends, p.B, i);
+    int32_t* entry = p.page_table + (size_t)b * p.max_pages + pages_of(news[b]) + i - (b ? ends[b - 1] : 0);
+    const int at = n_free + total - 1 - i;
+    if (at < p.free_cap) p.free_pages[at] = *entry;
+    *entry = -1;
+  }
+  cluster_wait();
+  if (cta != 0) return;
+  for (int b = tid; b < p.B; b += PLAN_THREADS) p.len[b] = news[b];
+  if (tid == 0) *p.n_free = min(n_free + total, p.free_cap);
+}
+
+// ---------------------------------------------------------------------------------------------
+// append
+// ---------------------------------------------------------------------------------------------
+
+struct AppendParams {
+  const char *k, *v;
+  long long k_row, k_head, v_row, v_head;      // bytes
+  const int32_t* slot;
+  char *k_pool, *v_pool, *k_min, *k_max;
+  int T, H, block;
+  long long n_slots;
+};
+
+// Smaller / larger of each pair, a NaN if there is one.
+__device__ __forceinline__ uint32_t lower(uint32_t a, uint32_t b, bf16) {
+  uint32_t r;
+  asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t upper(uint32_t a, uint32_t b, bf16) {
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t lower(uint32_t a, uint32_t b, float) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)));
+  return __float_as_uint(r);
+}
+__device__ __forceinline__ uint32_t upper(uint32_t a, uint32_t b, float) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)));
+  return __float_as_uint(r);
+}
+
+// A run is what follows one another in the list within one page.  LANES threads own a run of one head, each 16 bytes of the head:
+// a run has one owner, so the page's minimum and maximum need no atomics and do not depend on any order.  All of a run's rows are
+// in flight at once.  Keys and values are for different threads (blockIdx.y).
+template <typename T, int DH>
+__global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams p) {
+  constexpr int LANES = DH * (int)sizeof(T) / 16, ROW = DH * (int)sizeof(T);
+  const int lane = threadIdx.x % LANES;
+  const long long item = ((long long)blockIdx.x * 256 + threadIdx.x) / LANES;
+  const int h = (int)(item % p.H);
+  const long long t0 = item / p.H * p.block;
+  const bool values = blockIdx.y != 0;
+  const char* src = (values ? p.v + h * p.v_head : p.k + h * p.k_head) + lane * 16;
+  const long long row = values ? p.v_row : p.k_row;
+  char* pool = (values ? p.v_pool : p.k_pool) + lane * 16;
+  const bool sums = !values && p.k_min != nullptr;
+  griddep_wait();
+  griddep_launch();
+  for (long long t = t0; t < min((long long)p.T, t0 + p.block); ++t) {
+    const int s0 = p.slot[t];
+    if (s0 < 0 || s0 >= p.n_slots) continue;
+    const int page = s0 / CERB_PAGE;
+    if (t > 0) {
+      const int before = p.slot[t - 1];
+      if (before >= 0 && before / CERB_PAGE == page) continue;           // its owner is that one's
+    }
+    uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+    bool fresh = false, first = true;
+    char* at = sums ? p.k_min + ((size_t)page * p.H + h) * ROW + lane * 16 : nullptr;
+    char* at_hi = sums ? p.k_max + ((size_t)page * p.H + h) * ROW + lane * 16 : nullptr;
+    // (a run is at most a page long if no slot comes twice)
+    for (long long u = t;; u += CERB_PAGE) {
+      int off[CERB_PAGE];
+      uint4 x[CERB_PAGE];
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < CERB_PAGE; ++i) {
+        const int s = u + i < p.T ? p.slot[u + i] : -1;
+        off[i] = s >= 0 && s / CERB_PAGE == page ? s % CERB_PAGE : -1;
+      }
+#pragma unroll
+      for (int i = 0; i < CERB_PAGE; ++i) {
+        if (n == i && off[i] >= 0) ++n;
+        if (i < n) x[i] = *reinterpret_cast<const uint4*>(src + (u + i) * row);
+      }
+#pragma unroll
+      for (int i = 0; i < CERB_PAGE; ++i) {
+        if (i >= n) continue;
+        *reinterpret_cast<uint4*>(pool + (((size_t)page * p.H + h) * CERB_PAGE + off[i]) * ROW) = x[i];
+        if (!sums) continue;
+        fresh |= off[i] == 0;
+        if (first) { lo = hi = x[i]; first = false; continue; }
+        lo = make_uint4(lower(lo.x, x[i].x, T()), lower(lo.y, x[i].y, T()), lower(lo.z, x[i].z, T()), lower(lo.w, x[i].w, T()));
+        hi = make_uint4(upper(hi.x, x[i].x, T()), upper(hi.y, x[i].y, T()), upper(hi.z, x[i].z, T()), upper(hi.w, x[i].w, T()));
+      }
+      if (n < CERB_PAGE) break;
+    }
+    if (!sums) continue;
+    if (!fresh) {
+      const uint4 a = *reinterpret_cast<const uint4*>(at), b = *reinterpret_cast<const uint4*>(at_hi);
+      lo = make_uint4(lower(lo.x, a.x, T()), lower(lo.y, a.y, T()), lower(lo.z, a.z, T()), lower(lo.w, a.w, T()));
+      hi = make_uint4(upper(hi.x, b.x, T()), upper(hi.y, b.y, T()), upper(hi.z, b.z, T()), upper(hi.w, b.w, T()));
+    }
+    *reinterpret_cast<uint4*>(at) = lo;
+    *reinterpret_cast<uint4*>(at_hi) = hi;
+  }
+}
+
+int check_pages(const cerb_pages* s) {
+  if (!s || s->B < 0 || s->max_pages < 1 || s->free_cap < 0) return CERB_E_ARG;
+  if ((s->B && (!s->len || !s->page_table)) || (s->free_cap && !s->free_pages) || !s->n_free) return CERB_E_ARG;
+  if (s->B > kMaxRequests || s->max_pages > (1 << 26) || (long long)s->B * s->max_pages > 0x7fffffffll) return CERB_E_SHAPE;
+  return CERB_OK;
+}
+
+PagesParams pages_params(const cerb_pages* s) {
+  PagesParams p;
+  memset(&p, 0, sizeof(p));
+  p.len = s->len;
+  p.page_table = s->page_table;
+  p.free_pages = s->free_pages;
+  p.n_free = s->n_free;
+  p.B = s->B;
+  p.max_pages = s->max_pages;
+  p.free_cap = s->free_cap;
+  return p;
+}
+
+}  // namespace
+
+}  // namespace cerb
+
+using namespace cerb;
+
+extern "C" {
+
+int cerb_pages_plan(const cerb_pages* s, const int32_t* n_new, int32_t rows, int32_t* slot, int32_t* pos, int32_t* seq, int32_t* row_off,
+                    int32_t* granted, void* stream) {
+  CERB_TRY(check_pages(s));
+  if ((s->B && (!n_new || !granted)) || !row_off || rows < 0 || (rows && (!slot || !pos || !seq))) return CERB_E_ARG;
+  if (rows > (1 << 30)) return CERB_E_SHAPE;
+  PagesParams p = pages_params(s);
+  p.n_new = n_new;
+  p.slot = slot;
+  p.pos = pos;
+  p.seq = seq;
+  p.row_off = row_off;
+  p.granted = granted;
+  p.rows = rows;
+  const size_t smem = 4 * (size_t)p.B * sizeof(int);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (rows <= kPlanRowsOneCta) {
+    static std::atomic<uint64_t> done{0};
+    CERB_TRY(allow_smem(pages_plan_kernel<false>, done, 4 * kMaxRequests * (int)sizeof(int)));
+    return launch_pdl(pages_plan_kernel<false>, dim3(1), dim3(PLAN_THREADS), smem, st, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
+  }
+  static std::atomic<uint64_t> done{0};
+  CERB_TRY(allow_smem(pages_plan_kernel<true>, done, 4 * kMaxRequests * (int)sizeof(int)));
+  return launch_pdl_cluster(pages_plan_kernel<true>, dim3(PLAN_CLUSTER), dim3(PLAN_THREADS), smem, st, PLAN_CLUSTER, p) == cudaSuccess
+             ? CERB_OK : CERB_E_CUDA;
+}
+
+int cerb_pages_trim(const cerb_pages* s, const int32_t* keep, void* stream) {
+  CERB_TRY(check_pages(s));
+  if (s->B == 0) return CERB_OK;
+  if (!keep) return CERB_E_ARG;
+  PagesParams p = pages_params(s);
+  p.n_new = keep;
+  static std::atomic<uint64_t> done{0};
+  CERB_TRY(allow_smem(pages_trim_kernel, done, 2 * kMaxRequests * (int)sizeof(int)));
+  return launch_pdl_cluster(pages_trim_kernel, dim3(PLAN_CLUSTER), dim3(PLAN_THREADS), 2 * (size_t)p.B * sizeof(int), (cudaStream_t)stream,
+                            PLAN_CLUSTER, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
+}
+
+int cerb_kv_append(const cerb_kv_append_args* a, void* stream) {
+  if (!a || !a->k_min != !a->k_max) return CERB_E_ARG;
+  if (a->T > 0 && (!a->k || !a->v || !a->slot || !a->k_pool || !a->v_pool)) return CERB_E_ARG;
+  if ((a->dtype != CERB_F32 && a->dtype != CERB_BF16) || a->T < 0) return CERB_E_ARG;
+  if (a->n_kv_heads < 1 || (a->head_dim != 64 && a->head_dim != 128) || a->n_pool_pages < 1 || a->n_pool_pages > (1 << 27) - 1) return CERB_E_SHAPE;
+  const int es = a->dtype == CERB_BF16 ? 2 : 4;
+  const long long strides[4] = {a->k_row_stride, a->k_head_stride, a->v_row_stride, a->v_head_stride};
+  for (long long x : strides)
+    if (x * es % 16) return CERB_E_ARG;
+  if (((uintptr_t)a->k | (uintptr_t)a->v | (uintptr_t)a->k_pool | (uintptr_t)a->v_pool | (uintptr_t)a->k_min | (uintptr_t)a->k_max) & 15) return CERB_E_ARG;
+  if (a->T == 0) return CERB_OK;
+  AppendParams p;
+  p.k = (const char*)a->k;
+  p.v = (const char*)a->v;
+  p.k_row = a->k_row_stride * es;
+  p.k_head = a->k_head_stride * es;
+  p.v_row = a->v_row_stride * es;
+  p.v_head = a->v_head_stride * es;
+  p.slot = a->slot;
+  p.k_pool = (char*)a->k_pool;
+  p.v_pool = (char*)a->v_pool;
+  p.k_min = (char*)a->k_min;
+  p.k_max = (char*)a->k_max;
+  p.T = a->T;
+  p.H = a->n_kv_heads;
+  p.n_slots = (long long)a->n_pool_pages * CERB_PAGE;
+  // a token to a group of threads while they all fit the GPU at once, else as many as make it fit, a page at most
+  const long long lanes = a->head_dim * es / 16, threads = 2 * (long long)p.T * p.H * lanes, room = 148ll * 2048;
+  p.block = (int)((threads + room - 1) / room);
+  if (p.block > CERB_PAGE) p.block = CERB_PAGE;
+  const long long groups = ((long long)p.T + p.block - 1) / p.block * p.H, ctas = (groups * lanes + 255) / 256;
+  if (ctas > 0x7fffffffll) return CERB_E_SHAPE;
+  const dim3 grid((unsigned)ctas, 2);
+  auto kern = a->dtype == CERB_BF16 ? (a->head_dim == 128 ? kv_append_kernel<bf16, 128> : kv_append_kernel<bf16, 64>)
+                                    : (a->head_dim == 128 ? kv_append_kernel<float, 128> : kv_append_kernel<float, 64>);
+  return launch_pdl(kern, grid, dim3(256), 0, (cudaStream_t)stream, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
+}
+
+}  // extern "C"
