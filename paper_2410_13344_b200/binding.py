@@ -7,6 +7,7 @@ shared library has not been built -- there is no fallback path.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Dict, List, NamedTuple, Optional, Sequence
 
@@ -536,33 +537,33 @@ def gemm(X: torch.Tensor, W: torch.Tensor, scratch: Optional[torch.Tensor] = Non
 # ---- paged-cache operators of a serving loop (see the section on them in cerb.h)
 
 
-def _refuse(code: int, what: str, why: str):
+def _refuse(what: str, why: str, code: int = E_ARG):
     e = CerbError(code, what)
     e.args = ("%s: %s" % (e.args[0], why),)
     raise e
 
 
-def _need(ok: bool, what: str, why: str):
-    if not ok:
-        _refuse(E_ARG, what, why)
-
-
-def _on_device(what: str, device: torch.device, *tensors):
-    """All of them in that GPU's memory, whole numbers (dtype int32) in one piece."""
-    _need(device.type == "cuda", what, "tensors must be on a GPU")
+# (a call's checks are written for their cost: an attribute of a tensor is 0.06 to 0.2 us, and a step makes several calls a layer)
+def _index_tensors(what: str, device: int, tensors) -> None:
+    """Lengths, tables, lists and counts: int32, in one piece, on that GPU."""
+    if device < 0:
+        _refuse(what, "tensors must be on a GPU")
     for t in tensors:
-        _need(t.device == device, what, "tensors are on different devices")
-        _need(t.dtype == torch.int32 and t.is_contiguous(), what, "lengths, tables, lists and counts are contiguous int32 tensors")
+        if t.dtype is not torch.int32 or not t.is_contiguous():
+            _refuse(what, "lengths, tables, lists and counts are contiguous int32 tensors")
+        if t.get_device() != device:
+            _refuse(what, "tensors are on different devices")
 
 
-def _call(fn, what: str, device: torch.device, *args):
+def _call(fn, what: str, device: int, *args) -> None:
     """On the tensors' own device, and the stream that is current there."""
-    if device.index == torch.cuda.current_device():
+    if device == torch.cuda.current_device():
         rc = fn(*args, _stream())
     else:
         with torch.cuda.device(device):
             rc = fn(*args, _stream())
-    _check(rc, what)
+    if rc != OK:
+        raise CerbError(rc, what)
 
 
 class PagePlan(NamedTuple):
@@ -573,123 +574,141 @@ class PagePlan(NamedTuple):
     granted: torch.Tensor        # [B] tokens that a request got room for: all it wanted, or 0
 
 
-def _pages(what: str, n: torch.Tensor, lens, page_table, free_pages, n_free) -> Pages:
-    _on_device(what, lens.device, n, lens, page_table, free_pages, n_free)
+def _pages(what: str, device: int, n: torch.Tensor, lens, page_table, free_pages, n_free) -> Pages:
+    _index_tensors(what, device, (n, lens, page_table, free_pages, n_free))
     B = lens.numel()
-    _need(lens.dim() == 1 and n.shape == lens.shape and page_table.dim() == 2 and page_table.shape[0] == B and free_pages.dim() == 1
-          and n_free.numel() == 1, what, "lens [B], one number a request, page_table [B][max_pages], free_pages [capacity], n_free [1]")
-    _need(page_table.shape[1] >= 1, what, "a table has one column at least")
-    return Pages(B, page_table.shape[1], free_pages.numel(), lens.data_ptr(), page_table.data_ptr(), free_pages.data_ptr(), n_free.data_ptr())
+    table = page_table.shape
+    if lens.dim() != 1 or n.shape != lens.shape or len(table) != 2 or table[0] != B or table[1] < 1 or free_pages.dim() != 1 or n_free.numel() != 1:
+        _refuse(what, "lens [B], a number a request, page_table [B][one column at least], free_pages [capacity], n_free [1]")
+    return Pages(B, table[1], free_pages.numel(), lens.data_ptr(), page_table.data_ptr(), free_pages.data_ptr(), n_free.data_ptr())
 
 
 def pages_plan(n_new: torch.Tensor, lens: torch.Tensor, page_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor,
                rows: int) -> PagePlan:
     """Room for n_new[b] more tokens of every request, in place: lens, page_table, free_pages and n_free are the state of the cache
     (see cerb_pages_plan); `rows` rows of a step's buffers describe the new tokens."""
-    _need(rows >= 0, "cerb_pages_plan", "rows is negative")
-    a = _pages("cerb_pages_plan", n_new, lens, page_table, free_pages, n_free)
-    if a.B > 8192 or rows > 1 << 30:                         # (ahead of the allocation)
-        _refuse(E_SHAPE, "cerb_pages_plan", "more than 8192 requests or 2^30 rows")
-    pad = (rows + 3) // 4 * 4
-    out = torch.empty(3 * pad + 2 * a.B + 1, dtype=torch.int32, device=lens.device)
+    what, device = "cerb_pages_plan", lens.get_device()
+    a = _pages(what, device, n_new, lens, page_table, free_pages, n_free)
+    B = a.B
+    if rows < 0:
+        _refuse(what, "rows is negative")
+    if B > 8192 or rows > 1 << 30:                           # (ahead of the allocation)
+        _refuse(what, "more than 8192 requests or 2^30 rows", E_SHAPE)
+    out = torch.empty(3 * rows + 2 * B + 1, dtype=torch.int32, device=lens.device)
     at = out.data_ptr()
-    p = PagePlan(out[:rows], out[pad:pad + rows], out[2 * pad:2 * pad + rows], out[3 * pad:3 * pad + a.B + 1], out[3 * pad + a.B + 1:])
-    _call(lib().cerb_pages_plan, "cerb_pages_plan", lens.device, C.byref(a), n_new.data_ptr(), rows, at, at + 4 * pad, at + 8 * pad, at + 12 * pad,
-          at + 12 * pad + 4 * (a.B + 1))
-    return p
+    _call(lib().cerb_pages_plan, what, device, C.byref(a), n_new.data_ptr(), rows, at, at + 4 * rows, at + 8 * rows, at + 12 * rows,
+          at + 12 * rows + 4 * (B + 1))
+    return PagePlan(*out.split((rows, rows, rows, B + 1, B)))
 
 
 def pages_trim(keep: torch.Tensor, lens: torch.Tensor, page_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor) -> None:
     """Cuts every request down to keep[b] tokens and gives its other pages back, in place (see cerb_pages_trim)."""
-    a = _pages("cerb_pages_trim", keep, lens, page_table, free_pages, n_free)
-    _call(lib().cerb_pages_trim, "cerb_pages_trim", lens.device, C.byref(a), keep.data_ptr())
+    device = lens.get_device()
+    a = _pages("cerb_pages_trim", device, keep, lens, page_table, free_pages, n_free)
+    _call(lib().cerb_pages_trim, "cerb_pages_trim", device, C.byref(a), keep.data_ptr())
 
 
 _DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
 
 
-def _rows(what: str, name: str, t: torch.Tensor, heads: int, head_dim: int):
+def _pair(what: str, names: str, a: torch.Tensor, b: torch.Tensor, dims: int) -> int:
+    """dtype code of two tensors of a cache, alike and contiguous."""
+    if a.dim() != dims or a.shape != b.shape or not a.is_contiguous() or not b.is_contiguous():
+        _refuse(what, names + " (alike, contiguous)")
+    dt = a.dtype
+    if dt not in _DTYPES or b.dtype is not dt:
+        _refuse(what, "bfloat16 or float32, and no mixture")
+    if a.get_device() != b.get_device():
+        _refuse(what, "tensors are on different devices")
+    return _DTYPES[dt]
+
+
+_POOLS = "pools are [pages][KV heads][16][head_dim]"
+_SUMMARIES = "k_min and k_max are [pages][KV heads][head_dim]"
+
+
+def _rows(what: str, name: str, t: torch.Tensor, rows: int, heads: int, head_dim: int, like: torch.Tensor, device: int):
     """(row stride, head stride) of a [rows][heads][head_dim] operand."""
-    _need(t.dim() == 3 and t.shape[1] == heads and t.shape[2] == head_dim and t.stride(2) == 1, what,
-          "%s is [rows][%d][%d], the elements of a head next to one another" % (name, heads, head_dim))
-    return t.stride(0), t.stride(1)
-
-
-def _pools(what: str, *pools) -> tuple:
-    """(pages, KV heads, head_dim, dtype code) of pools [pages][KV heads][16][head_dim]."""
-    k = pools[0]
-    _need(k.dim() == 4 and k.shape[2] == PAGE, what, "pools are [pages][KV heads][16][head_dim]")
-    for t in pools:
-        _need(t.shape == k.shape and t.dtype == k.dtype and t.device == k.device and t.is_contiguous(), what, "the pools are alike and contiguous")
-    _need(k.dtype in _DTYPES, what, "bfloat16 or float32")
-    return k.shape[0], k.shape[1], k.shape[3], _DTYPES[k.dtype]
-
-
-def _summaries(what: str, k_min, k_max, dtype, device):
-    _need(k_min.dim() == 3 and k_min.shape == k_max.shape and k_min.is_contiguous() and k_max.is_contiguous(), what,
-          "k_min and k_max are [pages][KV heads][head_dim]")
-    _need(k_min.dtype == dtype and k_max.dtype == dtype and k_min.device == device and k_max.device == device, what,
-          "k_min and k_max have another type or device")
+    if t.shape != (rows, heads, head_dim) or t.dtype is not like.dtype or t.get_device() != device:
+        _refuse(what, "%s is [%d][%d][%d], of the cache's type and on its device" % (name, rows, heads, head_dim))
+    r, h, e = t.stride()
+    if e != 1:
+        _refuse(what, "the elements of a head of %s are next to one another" % name)
+    return r, h
 
 
 def kv_append(k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor,
               k_min: Optional[torch.Tensor] = None, k_max: Optional[torch.Tensor] = None) -> None:
     """Writes k and v [T][KV heads][head_dim] (views into a packed product will do) into their slots of the pools, and keeps the pages' minima and
     maxima (see cerb_kv_append)."""
-    what = "cerb_kv_append"
-    n_pages, Hk, D, dt = _pools(what, k_pool, v_pool)
-    _on_device(what, k_pool.device, slot)
+    what, device = "cerb_kv_append", k_pool.get_device()
+    dt = _pair(what, _POOLS, k_pool, v_pool, 4)
+    n_pages, Hk, page, D = k_pool.shape
+    if page != PAGE:
+        _refuse(what, _POOLS)
+    _index_tensors(what, device, (slot,))
     T = slot.numel()
-    kr, kh = _rows(what, "k", k, Hk, D)
-    vr, vh = _rows(what, "v", v, Hk, D)
-    _need(k.shape[0] == T and v.shape[0] == T, what, "a slot for every row")
-    _need(k.dtype == v.dtype == k_pool.dtype and k.device == v.device == k_pool.device, what, "k, v and the pools differ in type or device")
-    _need((k_min is None) == (k_max is None), what, "k_min and k_max come together")
-    if k_min is not None:
-        _summaries(what, k_min, k_max, k_pool.dtype, k_pool.device)
-        _need(k_min.shape == (n_pages, Hk, D), what, "k_min and k_max are of other pages than the pools")
-    a = KvAppendArgs(dt, T, Hk, D, k.data_ptr(), v.data_ptr(), kr, kh, vr, vh, slot.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), _ptr(k_min),
-                     _ptr(k_max), n_pages)
-    _call(lib().cerb_kv_append, what, k_pool.device, C.byref(a))
+    kr, kh = _rows(what, "k", k, T, Hk, D, k_pool, device)
+    vr, vh = _rows(what, "v", v, T, Hk, D, k_pool, device)
+    lo = hi = None
+    if k_min is not None or k_max is not None:
+        if k_min is None or k_max is None:
+            _refuse(what, "k_min and k_max come together")
+        if _pair(what, _SUMMARIES, k_min, k_max, 3) != dt or k_min.shape != (n_pages, Hk, D) or k_min.get_device() != device:
+            _refuse(what, "k_min and k_max are of other pages than the pools, or of another type")
+        lo, hi = k_min.data_ptr(), k_max.data_ptr()
+    a = KvAppendArgs(dt, T, Hk, D, k.data_ptr(), v.data_ptr(), kr, kh, vr, vh, slot.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), lo, hi, n_pages)
+    _call(lib().cerb_kv_append, what, device, C.byref(a))
 
 
-def _queries(what: str, q, Hk: int, D: int, dtype, device, page_table, lens):
-    _need(q.dim() == 3 and q.shape[1] >= 1 and Hk >= 1 and q.shape[1] % Hk == 0, what, "q is [B][heads][head_dim], its heads a multiple of the KV heads")
-    _need(q.dtype == dtype and q.device == device, what, "q and the cache differ in type or device")
-    _on_device(what, device, page_table, lens)
-    B = q.shape[0]
-    _need(lens.shape == (B,) and page_table.dim() == 2 and page_table.shape[0] == B and page_table.shape[1] >= 1, what,
-          "a length and a row of the page table for every sequence")
-    return _rows(what, "q", q, q.shape[1], D)
+def _queries(what: str, q: torch.Tensor, Hk: int, D: int, like: torch.Tensor, device: int, page_table, lens):
+    """(B, heads, row stride, head stride, columns of the page table)"""
+    shape, table = q.shape, page_table.shape
+    if len(shape) != 3 or Hk < 1 or shape[1] < 1 or shape[1] % Hk:
+        _refuse(what, "q is [B][heads][head_dim], its heads a multiple of the KV heads")
+    B, H = shape[0], shape[1]
+    if len(table) != 2 or table[0] != B or table[1] < 1 or lens.shape != (B,):
+        _refuse(what, "a length and a row of the page table for every sequence")
+    _index_tensors(what, device, (page_table, lens))
+    r, h = _rows(what, "q", q, B, H, D, like, device)
+    return B, H, r, h, table[1]
 
 
-def _scratch(what: str, given: Optional[torch.Tensor], need: int, device) -> Optional[torch.Tensor]:
+def _scratch(what: str, given: Optional[torch.Tensor], need: int, device: int):
+    """(address, bytes, what keeps it alive) of the scratch."""
     if given is None:
-        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    _need(given.device == device and given.is_contiguous() and given.dtype == torch.uint8, what, "scratch is a contiguous uint8 tensor on the same device")
-    return given
+        if not need:
+            return None, 0, None
+        given = torch.empty(need, dtype=torch.uint8, device=device)
+    elif given.get_device() != device or given.dtype is not torch.uint8 or not given.is_contiguous():
+        _refuse(what, "scratch is a contiguous uint8 tensor on the same device")
+    return given.data_ptr(), given.numel(), given
+
+
+@functools.lru_cache(maxsize=256)
+def _scratch_bytes(fn: str, *sizes: int) -> int:
+    """(a function of the sizes alone)"""
+    nb = C.c_size_t(0)
+    _check(getattr(lib(), fn)(*sizes, C.byref(nb)), fn)
+    return nb.value
 
 
 def page_select(q: torch.Tensor, k_min: torch.Tensor, k_max: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor, n_pages: int, max_len: int,
                 n_first: int = 1, n_last: int = 1, scratch: Optional[torch.Tensor] = None):
     """The n_pages pages of every (sequence, KV head) that hold the largest upper bounds of q . k, the first n_first and the last n_last always among
     them (see cerb_page_select).  Returns (sel [B][KV heads][n_pages] ascending and -1 behind, n_sel [B])."""
-    what = "cerb_page_select"
-    _need(k_min.dtype in _DTYPES, what, "bfloat16 or float32")
-    _summaries(what, k_min, k_max, k_min.dtype, k_min.device)
+    what, device = "cerb_page_select", k_min.get_device()
+    dt = _pair(what, _SUMMARIES, k_min, k_max, 3)
     P, Hk, D = k_min.shape
-    qr, qh = _queries(what, q, Hk, D, k_min.dtype, k_min.device, page_table, lens)
-    _need(n_pages >= 1 and n_first >= 0 and n_last >= 0 and max_len >= 1, what, "counts are not negative, n_pages and max_len one at least")
-    B, H, _ = q.shape
-    dt, mp = _DTYPES[q.dtype], page_table.shape[1]
-    nb = C.c_size_t(0)
-    _check(lib().cerb_page_select_scratch_bytes(dt, B, H, Hk, D, mp, max_len, C.byref(nb)), what)
-    scratch = _scratch(what, scratch, nb.value, q.device)
-    sel = torch.empty(B, Hk, n_pages, dtype=torch.int32, device=q.device)
-    n_sel = torch.empty(B, dtype=torch.int32, device=q.device)
+    B, H, qr, qh, mp = _queries(what, q, Hk, D, k_min, device, page_table, lens)
+    if n_pages < 1 or n_first < 0 or n_last < 0 or max_len < 1:
+        _refuse(what, "counts are not negative, n_pages and max_len one at least")
+    at, size, scratch = _scratch(what, scratch, _scratch_bytes("cerb_page_select_scratch_bytes", dt, B, H, Hk, D, mp, max_len), device)
+    sel = torch.empty((B, Hk, n_pages), dtype=torch.int32, device=device)
+    n_sel = torch.empty(B, dtype=torch.int32, device=device)
     a = PageSelectArgs(dt, B, H, Hk, D, mp, P, q.data_ptr(), qr, qh, k_min.data_ptr(), k_max.data_ptr(), page_table.data_ptr(), lens.data_ptr(), n_pages,
-                       n_first, n_last, max_len, sel.data_ptr(), n_sel.data_ptr(), _ptr(scratch), 0 if scratch is None else scratch.numel())
-    _call(lib().cerb_page_select, what, q.device, C.byref(a))
+                       n_first, n_last, max_len, sel.data_ptr(), n_sel.data_ptr(), at, size)
+    _call(lib().cerb_page_select, what, device, C.byref(a))
     return sel, n_sel
 
 
@@ -698,25 +717,27 @@ def paged_attention(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor,
                     scratch: Optional[torch.Tensor] = None):
     """Attention of one new token per sequence, q [B][heads][head_dim] (a view into a packed product will do), over the paged cache, over its last
     `window` tokens, or over the pages of page_select's lists (see cerb_paged_attention).  Returns (out, lse)."""
-    what = "cerb_paged_attention"
-    n_pages, Hk, D, dt = _pools(what, k_pool, v_pool)
-    qr, qh = _queries(what, q, Hk, D, k_pool.dtype, k_pool.device, page_table, lens)
-    _need(max_len >= 1 and window >= 0, what, "max_len is one at least, window not negative")
-    B, H, _ = q.shape
-    _need((sel is None) == (n_sel is None), what, "sel and n_sel come together")
-    max_sel = 0
-    if sel is not None:
-        _on_device(what, q.device, sel, n_sel)
-        _need(sel.dim() == 3 and sel.shape[0] == B and sel.shape[1] == Hk and sel.shape[2] >= 1 and n_sel.shape == (B,), what,
-              "sel is [B][KV heads][pages], n_sel [B]")
-        max_sel = sel.shape[2]
-    nb = C.c_size_t(0)
-    _check(lib().cerb_paged_attention_scratch_bytes(dt, B, H, Hk, D, max_len, window, max_sel, C.byref(nb)), what)
-    scratch = _scratch(what, scratch, nb.value, q.device)
-    out = torch.empty(B, H, D, dtype=q.dtype, device=q.device)
-    lse = torch.empty(B, H, dtype=torch.float32, device=q.device) if want_lse else None
-    a = PagedAttnArgs(dt, B, H, Hk, D, page_table.shape[1], n_pages, q.data_ptr(), qr, qh, k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(),
-                      lens.data_ptr(), _ptr(sel), _ptr(n_sel), max_sel, out.data_ptr(), _ptr(lse), scale, max_len, window, _ptr(scratch),
-                      0 if scratch is None else scratch.numel())
-    _call(lib().cerb_paged_attention, what, q.device, C.byref(a))
+    what, device = "cerb_paged_attention", k_pool.get_device()
+    dt = _pair(what, _POOLS, k_pool, v_pool, 4)
+    n_pages, Hk, page, D = k_pool.shape
+    if page != PAGE:
+        _refuse(what, _POOLS)
+    B, H, qr, qh, mp = _queries(what, q, Hk, D, k_pool, device, page_table, lens)
+    if max_len < 1 or window < 0:
+        _refuse(what, "max_len is one at least, window not negative")
+    max_sel, sel_at, n_sel_at = 0, None, None
+    if sel is not None or n_sel is not None:
+        if sel is None or n_sel is None:
+            _refuse(what, "sel and n_sel come together")
+        _index_tensors(what, device, (sel, n_sel))
+        lists = sel.shape
+        if len(lists) != 3 or lists[0] != B or lists[1] != Hk or lists[2] < 1 or n_sel.shape != (B,):
+            _refuse(what, "sel is [B][KV heads][pages], n_sel [B]")
+        max_sel, sel_at, n_sel_at = lists[2], sel.data_ptr(), n_sel.data_ptr()
+    at, size, scratch = _scratch(what, scratch, _scratch_bytes("cerb_paged_attention_scratch_bytes", dt, B, H, Hk, D, max_len, window, max_sel), device)
+    out = torch.empty((B, H, D), dtype=q.dtype, device=device)
+    lse = torch.empty((B, H), dtype=torch.float32, device=device) if want_lse else None
+    a = PagedAttnArgs(dt, B, H, Hk, D, mp, n_pages, q.data_ptr(), qr, qh, k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(), lens.data_ptr(),
+                      sel_at, n_sel_at, max_sel, out.data_ptr(), _ptr(lse), scale, max_len, window, at, size)
+    _call(lib().cerb_paged_attention, what, device, C.byref(a))
     return out, lse

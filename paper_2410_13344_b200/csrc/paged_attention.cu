@@ -9,13 +9,16 @@
 #include <math.h>
 #include <string.h>
 
-#include "cerb_internal.cuh"
+#include <algorithm>
+
+#include "tc_common.cuh"
 
 namespace cerb {
 
 namespace {
 
 constexpr int PA_WARPS = 4;
+constexpr int PA_CLUSTER = 8;         // CTAs of a cluster at most
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct PagedParams {
@@ -23,11 +26,13 @@ struct PagedParams {
   const int32_t *page_table, *len, *sel, *n_sel;
   void* out;
   float* lse;
-  float *part_o, *part_ml;        // [unit][split][heads of a unit][Dh], [..][2]
+  float *part_o, *part_ml;        // [2 * CTAs][heads of a unit][Dh], [..][2]
+  int4* meta;                     // [joins]: unit, first part, number of parts (1 or less: nothing to join)
   long long q_row, q_head;        // elements
   int B, H, Hk, G, units_h;       // units_h: units per KV head (groups of more heads than a unit takes)
   int max_pages, n_pool_pages, max_sel, window;
-  int nsplit, chunk;              // splits and pages of one
+  int min_share, by_unit;         // by_unit: a join per unit, else one per CTA
+  int together;                   // CTAs of a cluster
   float scale_log2;
 };
 
@@ -44,7 +49,6 @@ __device__ __forceinline__ Span span_of(const PagedParams& p, int b) {
   if (s.hi == 0) s.items = 0;
   return s;
 }
-__device__ __forceinline__ int splits_of(const PagedParams& p, int items) { return min(p.nsplit, (items + p.chunk - 1) / p.chunk); }
 
 // The page of an item: its number among the sequence's, and where it lies (-1: nothing to read there).
 struct PageRef {
@@ -59,6 +63,102 @@ __device__ __forceinline__ PageRef page_ref(const PagedParams& p, const Span& s,
   if (at >= 0 && at < p.n_pool_pages) r.at = at;
   return r;
 }
+
+// ---- shares: the items of all sequences and heads one after another, cut into one share per CTA ----
+struct Share {
+  long long begin, end, size;   // items; of every CTA's share
+  int b;                        // the sequence that begin lies in,
+  long long off;                // and where in it
+};
+__device__ __forceinline__ Share share_of(const PagedParams& p) {
+  __shared__ long long s_sum[PA_WARPS], s_off;
+  __shared__ int s_b;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const bool few = p.B <= 32;                                            // every warp for itself
+  const int per = few ? 1 : (p.B + PA_WARPS * 32 - 1) / (PA_WARPS * 32);
+  const int b0 = min(p.B, (few ? lane : tid) * per), b1 = min(p.B, b0 + per);
+  const long long uh = (long long)p.Hk * p.units_h;
+  long long mine = 0;
+  for (int b = b0; b < b1; ++b) mine += span_of(p, b).items * uh;
+  long long sum = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long u = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += u;
+  }
+  long long total = __shfl_sync(0xffffffffu, sum, 31);
+  if (!few) {
+    if (lane == 31) s_sum[warp] = sum;
+    __syncthreads();
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < PA_WARPS; ++w) {
+      if (w < warp) sum += s_sum[w];
+      total += s_sum[w];
+    }
+  }
+  Share s;
+  const long long even = total >> 32 ? (total + gridDim.x - 1) / gridDim.x : ((unsigned)total + (gridDim.x - 1)) / gridDim.x;
+  s.size = max(even, (long long)p.min_share);
+  s.begin = min(total, s.size * blockIdx.x);
+  s.end = min(total, s.begin + s.size);
+  const bool here = s.begin >= sum - mine && s.begin < sum;
+  long long at = sum - mine;
+  int b = b0;
+  if (here)
+    for (;; ++b) {
+      const long long n = span_of(p, b).items * uh;
+      if (s.begin < at + n) break;
+      at += n;
+    }
+  if (few) {
+    const int from = max(__ffs(__ballot_sync(0xffffffffu, here)) - 1, 0);
+    s.b = __shfl_sync(0xffffffffu, b, from);
+    s.off = s.begin - __shfl_sync(0xffffffffu, at, from);
+  } else {
+    if (here) { s_b = b; s_off = s.begin - at; }
+    __syncthreads();
+    s.b = s_b;
+    s.off = s_off;
+  }
+  return s;
+}
+
+// The running maxima, sums and unnormalised outputs of a CTA's warps.
+template <int DH, int HEADS>
+struct alignas(16) Sums {                                                // (written and sent in pieces of 8 bytes)
+  float o[PA_WARPS][HEADS][DH], m[PA_WARPS][HEADS], l[PA_WARPS][HEADS];
+};
+template <int DH, int HEADS>
+__device__ __forceinline__ float merge_warps(const Sums<DH, HEADS>& s, int h, int d, float& m, float& l) {
+  m = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < PA_WARPS; ++w) m = fmaxf(m, s.m[w][h]);
+  const float u = m == -INFINITY ? 0.f : m;
+  float o = 0.f;
+  l = 0.f;
+#pragma unroll
+  for (int w = 0; w < PA_WARPS; ++w) {
+    const float f = exp2f(s.m[w][h] - u);
+    l += s.l[w][h] * f;
+    o += s.o[w][h][d] * f;
+  }
+  return o;
+}
+// (a row without keys: zeros, and the logarithm of nothing)
+template <typename T>
+__device__ __forceinline__ void store_out(const PagedParams& p, size_t row, int d, int dh, float o, float m, float l) {
+  const float x = l > 0.f || l != l ? o / l : 0.f;
+  if constexpr (sizeof(T) == 2) reinterpret_cast<bf16*>(p.out)[row * dh + d] = __float2bfloat16_rn(x);
+  else reinterpret_cast<float*>(p.out)[row * dh + d] = x;
+  if (d == 0 && p.lse) p.lse[row] = (m + log2f(l)) * kLn2;
+}
+
+// A piece of a unit: some of its items, for these of the query heads.
+struct Piece {
+  Span sp;
+  int b, kvh, head0, heads, item0, item1;
+};
 
 __device__ __forceinline__ uint4 ld16(const void* src) {
   uint4 r;
@@ -76,193 +176,175 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   return r;
 }
 
-// One CTA's part (its running maximum, sum and unnormalised outputs per head) as result or as partial.
-// s_o [warp][head][DH], s_m and s_l [warp][head]
-template <typename T, int DH, int HEADS>
-__device__ __forceinline__ void finish_cta(const PagedParams& p, const float* s_o, const float* s_m, const float* s_l, int unit, int split, int live,
-                                           int b, int head0, int heads) {
-  __syncthreads();
-  for (int i = threadIdx.x; i < heads * DH; i += PA_WARPS * 32) {
-    const int h = i / DH, d = i % DH;
-    float m = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < PA_WARPS; ++w) m = fmaxf(m, s_m[w * HEADS + h]);
-    const float u = m == -INFINITY ? 0.f : m;
-    float l = 0.f, o = 0.f;
-#pragma unroll
-    for (int w = 0; w < PA_WARPS; ++w) {
-      const float f = exp2f(s_m[w * HEADS + h] - u);
-      l += s_l[w * HEADS + h] * f;
-      o += s_o[(w * HEADS + h) * DH + d] * f;
-    }
-    if (live > 1) {
-      const size_t at = ((size_t)unit * p.nsplit + split) * HEADS + h;
-      p.part_o[at * DH + d] = o;
-      if (d == 0) { p.part_ml[2 * at] = m; p.part_ml[2 * at + 1] = l; }
-    } else {
-      const size_t row = (size_t)b * p.H + head0 + h;
-      const float x = l > 0.f || l != l ? o / l : 0.f;                   // (a row without keys: zeros)
-      if constexpr (sizeof(T) == 2) reinterpret_cast<bf16*>(p.out)[row * DH + d] = __float2bfloat16_rn(x);
-      else reinterpret_cast<float*>(p.out)[row * DH + d] = x;
-      if (d == 0 && p.lse) p.lse[row] = (m + log2f(l)) * kLn2;
-    }
-  }
-}
 
 // bf16.  Both products have the keys (of K q: 16 keys; of V p: Dh) on the MMA's 16 rows and the heads, NT groups of eight, on its columns: S^T = K q^T,
 // out^T = V^T P^T.  The order of the k positions of a product is free as long as both operands have the same, so a lane's 16
 // bytes of a key row (8 consecutive elements) are what it needs of two MMAs, and what it loads of the values, 8 elements of each of four keys, is
-// interleaved into fragments by byte permutes.  S^T's sums become P^T's fragments by two 8 x 8 transpositions of 16-bit elements.
-// P is rounded to bf16 for the second product (each weight off by at most 2^-9 of itself, in turns up and down; the sum l is that of the unrounded
+// interleaved into fragments by byte permutes.  S^T's sums become P^T's fragments by 8 x 8 transpositions of 16-bit elements.
+// P is rounded to bf16 for the second product (each weight off by at most 2^-8 of itself, up or down; the sum l is that of the unrounded
 // ones); scores, maxima, sums and outputs are fp32.
+// A warp takes KP pages at a time, 8 KB of keys and values, and has the next ones on their way.
 template <int DH, int NT>
-__global__ void __launch_bounds__(PA_WARPS * 32, NT == 1 ? 4 : 2) paged_attn_bf16_kernel(const PagedParams p) {
-  constexpr int HEADS = 8 * NT, KC = DH / 32, VH = DH / 64;              // chunks of a key row, halves of a value row
-  __shared__ float s_o[PA_WARPS * HEADS * DH];
-  __shared__ float s_m[PA_WARPS * HEADS], s_l[PA_WARPS * HEADS];
+__device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c, Sums<DH, 8 * NT>& sums) {
+  constexpr int KC = DH / 32, VH = DH / 64, KP = 128 / DH;               // chunks of a key row, halves of a value row, pages at a time
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int split = blockIdx.x % p.nsplit, unit = blockIdx.x / p.nsplit;
-  const int part = unit % p.units_h, kvh = unit / p.units_h % p.Hk, b = unit / p.units_h / p.Hk;
-  griddep_wait();
-  griddep_launch();
-  const Span sp = span_of(p, b);
-  const int live = splits_of(p, sp.items);
-  if (split >= max(live, 1)) return;
-  const int head0 = kvh * p.G + part * HEADS, heads = min(HEADS, p.G - part * HEADS);
-  const bf16* kp = reinterpret_cast<const bf16*>(p.k_pool) + (size_t)kvh * CERB_PAGE * DH + g * DH + t * 8;
-  const bf16* vp = reinterpret_cast<const bf16*>(p.v_pool) + (size_t)kvh * CERB_PAGE * DH + 2 * t * DH + g * 8;
+  const bf16* kp = reinterpret_cast<const bf16*>(p.k_pool) + (size_t)c.kvh * CERB_PAGE * DH + g * DH + t * 8;
+  const bf16* vp = reinterpret_cast<const bf16*>(p.v_pool) + (size_t)c.kvh * CERB_PAGE * DH + 2 * t * DH + g * 8;
   const size_t page_elems = (size_t)p.Hk * CERB_PAGE * DH;
+  // this warp's items: every PA_WARPS-th; the pages of 32 of them are looked up at once
+  int i = 0, pages_l = -1, at_l = -1;
+  const int mine = max(0, (c.item1 - c.item0 - warp + PA_WARPS - 1) / PA_WARPS);
+  auto next = [&]() {
+    PageRef r{-1, -1};
+    while (i < mine) {
+      if (i % 32 == 0) {
+        const PageRef l = i + lane < mine ? page_ref(p, c.sp, c.b, c.kvh, c.item0 + (i + lane) * PA_WARPS + warp) : PageRef{-1, -1};
+        pages_l = l.page;
+        at_l = l.at;
+      }
+      r.page = __shfl_sync(0xffffffffu, pages_l, i % 32);
+      r.at = __shfl_sync(0xffffffffu, at_l, i % 32);
+      ++i;
+      if (r.at >= 0) break;                                              // (there is something to read of it)
+    }
+    return r;
+  };
+  PageRef now[KP], then[KP];
+#pragma unroll
+  for (int a = 0; a < KP; ++a) now[a] = next();
+  uint4 k[KP][2][KC], v[KP][4][VH];
+  auto load_k = [&](const PageRef (&r)[KP]) {
+#pragma unroll
+    for (int a = 0; a < KP; ++a)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int j = 0; j < KC; ++j) k[a][e][j] = KP == 1 || r[a].at >= 0 ? ld16(kp + r[a].at * page_elems + e * 8 * DH + 32 * j) : make_uint4(0, 0, 0, 0);
+  };
+  auto load_v = [&](const PageRef (&r)[KP]) {
+#pragma unroll
+    for (int a = 0; a < KP; ++a)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < VH; ++j)
+          v[a][e][j] = KP == 1 || r[a].at >= 0 ? ld16(vp + r[a].at * page_elems + ((e & 1) + 8 * (e >> 1)) * DH + 64 * j) : make_uint4(0, 0, 0, 0);
+  };
+  if (now[0].at >= 0) { load_k(now); load_v(now); }
   uint4 q[NT][KC];
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
     for (int j = 0; j < KC; ++j)
-      q[n][j] = 8 * n + g < heads
-                    ? *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(p.q) + (size_t)b * p.q_row + (size_t)(head0 + 8 * n + g) * p.q_head + 32 * j + 8 * t)
+      q[n][j] = 8 * n + g < c.heads
+                    ? *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(p.q) + (size_t)c.b * p.q_row + (size_t)(c.head0 + 8 * n + g) * p.q_head + 32 * j + 8 * t)
                     : make_uint4(0, 0, 0, 0);
-  uint4 k[2][KC], v[4][VH];
-  auto load_k = [&](int at) {
-#pragma unroll
-    for (int r = 0; r < 2; ++r)
-#pragma unroll
-      for (int j = 0; j < KC; ++j) k[r][j] = ld16(kp + at * page_elems + r * 8 * DH + 32 * j);
-  };
-  auto load_v = [&](int at) {
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int j = 0; j < VH; ++j) v[r][j] = ld16(vp + at * page_elems + ((r & 1) + 8 * (r >> 1)) * DH + 64 * j);
-  };
   float o[NT][4 * VH][4], m[NT][2], l[NT][2];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     m[n][0] = m[n][1] = -INFINITY;
     l[n][0] = l[n][1] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4 * VH; ++i)
+    for (int d = 0; d < 4 * VH; ++d)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[n][i][e] = 0.f;
+      for (int e = 0; e < 4; ++e) o[n][d][e] = 0.f;
   }
-  // this warp's items: every PA_WARPS-th of a split's chunk, and of those nsplit chunks on (none, unless a sequence is longer than the caller said)
-  const int per = p.chunk / PA_WARPS;                                    // (chunk is a multiple of PA_WARPS)
-  auto item_of = [&](int i) { return (split + i / per * p.nsplit) * p.chunk + i % per * PA_WARPS + warp; };
-  int i = 0, pages_l = -1, at_l = -1;
-  PageRef now{-1, -1};
-  // the next item that there is something to read of, or -1
-  auto next = [&]() {
-    PageRef r{-1, -1};
-    for (;;) {
-      if (item_of(i) >= sp.items) break;                                 // (items only grow)
-      if (i % 32 == 0) {
-        const PageRef mine = page_ref(p, sp, b, kvh, item_of(i + lane));
-        pages_l = mine.page;
-        at_l = mine.at;
-      }
-      r.page = __shfl_sync(0xffffffffu, pages_l, i % 32);
-      r.at = __shfl_sync(0xffffffffu, at_l, i % 32);
-      ++i;
-      if (r.at >= 0) break;
-    }
-    return r;
-  };
-  now = next();
-  if (now.at >= 0) { load_k(now.at); load_v(now.at); }
-  while (now.at >= 0) {
-    const PageRef then = next();
-    float s[NT][4];
+  while (now[0].at >= 0) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      // (two accumulators: the tensor cores cut a sum off at every step)
-      float a0[4] = {0.f, 0.f, 0.f, 0.f}, a1[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int a = 0; a < KP; ++a) then[a] = next();
+    float s[KP][NT][4];
 #pragma unroll
-      for (int j = 0; j < KC; ++j) {
-        mma_16816(a0, k[0][j].x, k[1][j].x, k[0][j].y, k[1][j].y, q[n][j].x, q[n][j].y);
-        mma_16816(a1, k[0][j].z, k[1][j].z, k[0][j].w, k[1][j].w, q[n][j].z, q[n][j].w);
-      }
+    for (int a = 0; a < KP; ++a)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[n][e] = (a0[e] + a1[e]) * p.scale_log2;
-    }
-    if (then.at >= 0) load_k(then.at);
-    const int row0 = now.page * CERB_PAGE;
-    if (row0 < sp.lo || row0 + CERB_PAGE > sp.hi) {
-      // the ends: whatever lies outside counts nothing, and is nothing (it may be infinite)
+      for (int n = 0; n < NT; ++n) {
+        // (two accumulators: the tensor cores cut a sum off at every step)
+        float a0[4] = {0.f, 0.f, 0.f, 0.f}, a1[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = row0 + g + 8 * (e >> 1);
-          if (r < sp.lo || r >= sp.hi) s[n][e] = -INFINITY;
+        for (int j = 0; j < KC; ++j) {
+          mma_16816(a0, k[a][0][j].x, k[a][1][j].x, k[a][0][j].y, k[a][1][j].y, q[n][j].x, q[n][j].y);
+          mma_16816(a1, k[a][0][j].z, k[a][1][j].z, k[a][0][j].w, k[a][1][j].w, q[n][j].z, q[n][j].w);
         }
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = row0 + 2 * t + (r & 1) + 8 * (r >> 1);
-        if (row < sp.lo || row >= sp.hi)
+        for (int e = 0; e < 4; ++e) s[a][n][e] = (a0[e] + a1[e]) * p.scale_log2;
+      }
+    if (then[0].at >= 0) load_k(then);
 #pragma unroll
-          for (int j = 0; j < VH; ++j) v[r][j] = make_uint4(0, 0, 0, 0);
+    for (int a = 0; a < KP; ++a) {
+      const int row0 = now[a].at >= 0 ? now[a].page * CERB_PAGE : c.sp.hi;
+      if (row0 < c.sp.lo || row0 + CERB_PAGE > c.sp.hi) {
+        // the ends: whatever lies outside counts nothing, and is nothing (it may be infinite)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = row0 + g + 8 * (e >> 1);
+            if (r < c.sp.lo || r >= c.sp.hi) s[a][n][e] = -INFINITY;
+          }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = row0 + 2 * t + (e & 1) + 8 * (e >> 1);
+          if (r < c.sp.lo || r >= c.sp.hi)
+#pragma unroll
+            for (int j = 0; j < VH; ++j) v[a][e][j] = make_uint4(0, 0, 0, 0);
+        }
       }
     }
-    uint32_t pb[NT][2];
+    uint32_t pb[KP][NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      float mx[2] = {fmaxf(s[n][0], s[n][2]), fmaxf(s[n][1], s[n][3])};
+      float mx[2] = {fmaxf(s[0][n][0], s[0][n][2]), fmaxf(s[0][n][1], s[0][n][3])};
+#pragma unroll
+      for (int a = 1; a < KP; ++a)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) mx[e] = fmaxf(mx[e], fmaxf(s[a][n][e], s[a][n][e + 2]));
 #pragma unroll
       for (int w = 4; w < 32; w <<= 1)
 #pragma unroll
         for (int e = 0; e < 2; ++e) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], w));
-      float a[2];
+      float f[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         mx[e] = fmaxf(mx[e], m[n][e]);
         const float u = mx[e] == -INFINITY ? 0.f : mx[e];
-        a[e] = exp2f(m[n][e] - u);
+        f[e] = exp2f(m[n][e] - u);
         m[n][e] = mx[e];
-        s[n][e] = exp2f(s[n][e] - u);
-        s[n][e + 2] = exp2f(s[n][e + 2] - u);
-        l[n][e] = l[n][e] * a[e] + s[n][e] + s[n][e + 2];
+        l[n][e] *= f[e];
+#pragma unroll
+        for (int a = 0; a < KP; ++a) {
+          s[a][n][e] = exp2f(s[a][n][e] - u);
+          s[a][n][e + 2] = exp2f(s[a][n][e + 2] - u);
+          l[n][e] += s[a][n][e] + s[a][n][e + 2];
+        }
       }
-      if (__any_sync(0xffffffffu, a[0] != 1.f || a[1] != 1.f)) {
+      if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
 #pragma unroll
-        for (int c = 0; c < 4 * VH; ++c)
+        for (int d = 0; d < 4 * VH; ++d)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[n][c][e] *= a[e & 1];
+          for (int e = 0; e < 4; ++e) o[n][d][e] *= f[e & 1];
       }
-      pb[n][0] = transpose8x8(pack_bf16(s[n][0], s[n][1]));
-      pb[n][1] = transpose8x8(pack_bf16(s[n][2], s[n][3]));
-    }
 #pragma unroll
-    for (int j = 0; j < VH; ++j) {
-      const uint32_t x[4][4] = {{v[0][j].x, v[0][j].y, v[0][j].z, v[0][j].w}, {v[1][j].x, v[1][j].y, v[1][j].z, v[1][j].w},
-                                {v[2][j].x, v[2][j].y, v[2][j].z, v[2][j].w}, {v[3][j].x, v[3][j].y, v[3][j].z, v[3][j].w}};
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const uint32_t a0 = __byte_perm(x[0][c], x[1][c], 0x5410), a1 = __byte_perm(x[0][c], x[1][c], 0x7632);
-        const uint32_t a2 = __byte_perm(x[2][c], x[3][c], 0x5410), a3 = __byte_perm(x[2][c], x[3][c], 0x7632);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) mma_16816(o[n][4 * j + c], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+      for (int a = 0; a < KP; ++a) {
+        pb[a][n][0] = transpose8x8(pack_bf16(s[a][n][0], s[a][n][1]));
+        pb[a][n][1] = transpose8x8(pack_bf16(s[a][n][2], s[a][n][3]));
       }
     }
-    if (then.at >= 0) load_v(then.at);
-    now = then;
+#pragma unroll
+    for (int a = 0; a < KP; ++a)
+#pragma unroll
+      for (int j = 0; j < VH; ++j) {
+        const uint32_t x[4][4] = {{v[a][0][j].x, v[a][0][j].y, v[a][0][j].z, v[a][0][j].w}, {v[a][1][j].x, v[a][1][j].y, v[a][1][j].z, v[a][1][j].w},
+                                  {v[a][2][j].x, v[a][2][j].y, v[a][2][j].z, v[a][2][j].w}, {v[a][3][j].x, v[a][3][j].y, v[a][3][j].z, v[a][3][j].w}};
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const uint32_t a0 = __byte_perm(x[0][d], x[1][d], 0x5410), a1 = __byte_perm(x[0][d], x[1][d], 0x7632);
+          const uint32_t a2 = __byte_perm(x[2][d], x[3][d], 0x5410), a3 = __byte_perm(x[2][d], x[3][d], 0x7632);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_16816(o[n][4 * j + d], a0, a1, a2, a3, pb[a][n][0], pb[a][n][1]);
+        }
+      }
+    if (then[0].at >= 0) load_v(then);
+#pragma unroll
+    for (int a = 0; a < KP; ++a) now[a] = then[a];
   }
 #pragma unroll
   for (int n = 0; n < NT; ++n)
@@ -270,19 +352,18 @@ __global__ void __launch_bounds__(PA_WARPS * 32, NT == 1 ? 4 : 2) paged_attn_bf1
     for (int e = 0; e < 2; ++e) {
 #pragma unroll
       for (int w = 4; w < 32; w <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], w);
-      const int h = warp * HEADS + 8 * n + 2 * t + e;
-      if (g == 0) { s_m[h] = m[n][e]; s_l[h] = l[n][e]; }
-      // accumulator c of half j: rows g and g + 8 of the MMA are the elements 2c and 2c + 1 of the lane's eight
+      const int h = 8 * n + 2 * t + e;
+      if (g == 0) { sums.m[warp][h] = m[n][e]; sums.l[warp][h] = l[n][e]; }
+      // accumulator d of half j: rows g and g + 8 of the MMA are the elements 2d and 2d + 1 of the lane's eight
 #pragma unroll
-      for (int c = 0; c < 4 * VH; ++c)
-        *reinterpret_cast<float2*>(&s_o[h * DH + (c >> 2) * 64 + 8 * g + 2 * (c & 3)]) = make_float2(o[n][c][e], o[n][c][e + 2]);
+      for (int d = 0; d < 4 * VH; ++d)
+        *reinterpret_cast<float2*>(&sums.o[warp][h][(d >> 2) * 64 + 8 * g + 2 * (d & 3)]) = make_float2(o[n][d][e], o[n][d][e + 2]);
     }
-  finish_cta<bf16, DH, HEADS>(p, s_o, s_m, s_l, unit, split, live, b, head0, heads);
 }
 
-// fp32: plain FMA.  A lane owns DH / 32 elements of every key and value, a warp takes eight keys at a time for up to GH heads.  The lanes' 8 GH partial sums
-// meet by halving (every exchange carries half of what is left: as many shuffles as sums), after which each lane has the scores of few keys to
-// take the exponential of; the weights come back by shuffles.
+// fp32: plain FMA.  A lane owns DH / 32 elements of every key and value, a warp takes KEYS keys at a time for up to GH heads and has the next ones on their way.
+// The lanes' KEYS x GH partial sums meet by halving (every exchange carries half of what is left: as many shuffles as sums), after which each lane has the
+// scores of few keys to take the exponential of; the weights come back by shuffles.
 template <int N>
 __device__ __forceinline__ void halve_sums(float (&x)[N], int lane) {
   int n = N;
@@ -304,177 +385,373 @@ __device__ __forceinline__ void halve_sums(float (&x)[N], int lane) {
 }
 
 template <int DH, int GH>
-__global__ void __launch_bounds__(PA_WARPS * 32) paged_attn_f32_kernel(const PagedParams p) {
-  constexpr int E = DH / 32, NV = 8 * GH, R = NV >= 32 ? NV / 32 : 1, REP = NV >= 32 ? 1 : 32 / NV, LPH = 32 / GH;       // sums of a lane at the end, lanes with the same one; lanes of a head
-  __shared__ float s_o[PA_WARPS * GH * DH];
-  __shared__ float s_m[PA_WARPS * GH], s_l[PA_WARPS * GH];
+__device__ __forceinline__ void attend_f32(const PagedParams& p, const Piece& c, Sums<DH, GH>& sums) {
+  constexpr int E = DH / 32, KEYS = DH == 64 && GH <= 2 ? 16 : 8, STEPS = CERB_PAGE / KEYS;
+  constexpr int NV = KEYS * GH, R = NV >= 32 ? NV / 32 : 1, REP = NV >= 32 ? 1 : 32 / NV, LPH = 32 / GH;   // sums of a lane at the end, lanes with the same one; lanes of a head
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int split = blockIdx.x % p.nsplit, unit = blockIdx.x / p.nsplit;
-  const int part = unit % p.units_h, kvh = unit / p.units_h % p.Hk, b = unit / p.units_h / p.Hk;
-  griddep_wait();
-  griddep_launch();
-  const Span sp = span_of(p, b);
-  const int live = splits_of(p, sp.items);
-  if (split >= max(live, 1)) return;
-  const int head0 = kvh * p.G + part * GH, heads = min(GH, p.G - part * GH);
   const size_t page_elems = (size_t)p.Hk * CERB_PAGE * DH;
-  const float* kp = reinterpret_cast<const float*>(p.k_pool) + (size_t)kvh * CERB_PAGE * DH + lane * E;
-  const float* vp = reinterpret_cast<const float*>(p.v_pool) + (size_t)kvh * CERB_PAGE * DH + lane * E;
+  const float* kp = reinterpret_cast<const float*>(p.k_pool) + (size_t)c.kvh * CERB_PAGE * DH + lane * E;
+  const float* vp = reinterpret_cast<const float*>(p.v_pool) + (size_t)c.kvh * CERB_PAGE * DH + lane * E;
   struct Row {
     float x[E];
   };
-  auto load_row = [](const float* src) {
-    Row r;
-    if constexpr (E == 4)
-      asm volatile("ld.global.L1::no_allocate.L2::256B.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(r.x[0]), "=f"(r.x[1]), "=f"(r.x[2]), "=f"(r.x[3]) : "l"(src) : "memory");
-    else
-      asm volatile("ld.global.L1::no_allocate.L2::256B.v2.f32 {%0, %1}, [%2];" : "=f"(r.x[0]), "=f"(r.x[1]) : "l"(src) : "memory");
-    return r;
+  auto load_rows = [&](Row (&r)[KEYS], const float* src) {
+#pragma unroll
+    for (int j = 0; j < KEYS; ++j) {
+      if constexpr (E == 4)
+        asm volatile("ld.global.L1::no_allocate.L2::256B.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(r[j].x[0]), "=f"(r[j].x[1]), "=f"(r[j].x[2]), "=f"(r[j].x[3]) : "l"(src + j * DH) : "memory");
+      else
+        asm volatile("ld.global.L1::no_allocate.L2::256B.v2.f32 {%0, %1}, [%2];" : "=f"(r[j].x[0]), "=f"(r[j].x[1]) : "l"(src + j * DH) : "memory");
+    }
   };
+  // this warp's steps: every PA_WARPS-th item, the parts of a page that have a live row
+  int i = 0, step = STEPS, pages_l = -1, at_l = -1;
+  const int mine = max(0, (c.item1 - c.item0 - warp + PA_WARPS - 1) / PA_WARPS);
+  PageRef page{-1, -1};
+  struct Step {
+    int row0;
+    long long at;                                                        // element of the pools, -1: none
+  };
+  auto next = [&]() {
+    for (;;) {
+      if (step == STEPS) {
+        if (i >= mine) return Step{0, -1};
+        if (i % 32 == 0) {
+          const PageRef l = i + lane < mine ? page_ref(p, c.sp, c.b, c.kvh, c.item0 + (i + lane) * PA_WARPS + warp) : PageRef{-1, -1};
+          pages_l = l.page;
+          at_l = l.at;
+        }
+        page.page = __shfl_sync(0xffffffffu, pages_l, i % 32);
+        page.at = __shfl_sync(0xffffffffu, at_l, i % 32);
+        ++i;
+        if (page.at < 0) continue;
+        step = 0;
+      }
+      const int row0 = page.page * CERB_PAGE + step * KEYS;
+      const long long at = (long long)(page.at * page_elems) + step * KEYS * DH;
+      ++step;
+      if (row0 < c.sp.hi && row0 + KEYS > c.sp.lo) return Step{row0, at};
+    }
+  };
+  Row k[KEYS], v[KEYS];
+  Step now = next();
+  if (now.at >= 0) { load_rows(k, kp + now.at); load_rows(v, vp + now.at); }
   float q[GH][E], o[GH][E];
 #pragma unroll
   for (int h = 0; h < GH; ++h)
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      q[h][e] = h < heads ? reinterpret_cast<const float*>(p.q)[(size_t)b * p.q_row + (size_t)(head0 + h) * p.q_head + lane * E + e] : 0.f;
+      q[h][e] = h < c.heads ? reinterpret_cast<const float*>(p.q)[(size_t)c.b * p.q_row + (size_t)(c.head0 + h) * p.q_head + lane * E + e] : 0.f;
       o[h][e] = 0.f;
     }
   float m = -INFINITY, l = 0.f;                                          // of head lane / LPH
-  const int per = p.chunk / PA_WARPS;
-  for (int i = 0;; ++i) {
-    const int item = (split + i / per * p.nsplit) * p.chunk + i % per * PA_WARPS + warp;
-    if (item >= sp.items) break;
-    const PageRef r = page_ref(p, sp, b, kvh, item);
-    if (r.at < 0) continue;
+  while (now.at >= 0) {
+    const Step then = next();
+    float s[NV];                                                         // [head][key]
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int row0 = r.page * CERB_PAGE + half * 8;
-      if (row0 >= sp.hi || row0 + 8 <= sp.lo) continue;
-      Row k[8], v[8];
+    for (int h = 0; h < GH; ++h)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) k[j] = load_row(kp + r.at * page_elems + (half * 8 + j) * DH);
+      for (int j = 0; j < KEYS; ++j) {
+        float x = 0.f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = load_row(vp + r.at * page_elems + (half * 8 + j) * DH);
-      float s[NV];                                                       // [head][key]
-#pragma unroll
-      for (int h = 0; h < GH; ++h)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float x = 0.f;
-#pragma unroll
-          for (int e = 0; e < E; ++e) x = fmaf(q[h][e], k[j].x[e], x);
-          s[h * 8 + j] = x;
-        }
-      halve_sums(s, lane);
-      float mx = m;
-      const bool ends = row0 < sp.lo || row0 + 8 > sp.hi;
-#pragma unroll
-      for (int c = 0; c < R; ++c) {
-        s[c] *= p.scale_log2;
-        const int row = row0 + (lane / REP * R + c) % 8;
-        if (ends && (row < sp.lo || row >= sp.hi)) s[c] = -INFINITY;
-        mx = fmaxf(mx, s[c]);
+        for (int e = 0; e < E; ++e) x = fmaf(q[h][e], k[j].x[e], x);
+        s[h * KEYS + j] = x;
       }
-      if (ends) {
+    if (then.at >= 0) load_rows(k, kp + then.at);
+    halve_sums(s, lane);
+    const bool ends = now.row0 < c.sp.lo || now.row0 + KEYS > c.sp.hi;
+    float mx = m;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (row0 + j < sp.lo || row0 + j >= sp.hi)
+    for (int r = 0; r < R; ++r) {
+      s[r] *= p.scale_log2;
+      const int row = now.row0 + (lane / REP * R + r) % KEYS;
+      if (ends && (row < c.sp.lo || row >= c.sp.hi)) s[r] = -INFINITY;
+      mx = fmaxf(mx, s[r]);
+    }
+    if (ends) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[j].x[e] = 0.f;
-      }
+      for (int j = 0; j < KEYS; ++j)
+        if (now.row0 + j < c.sp.lo || now.row0 + j >= c.sp.hi)
 #pragma unroll
-      for (int w = 1; w < LPH; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-      const float u = mx == -INFINITY ? 0.f : mx, a = exp2f(m - u);
-      m = mx;
-      l *= a;
+          for (int e = 0; e < E; ++e) v[j].x[e] = 0.f;
+    }
 #pragma unroll
-      for (int c = 0; c < R; ++c) {
-        s[c] = exp2f(s[c] - u);
-        if (lane % REP == 0) l += s[c];
-      }
+    for (int w = 1; w < LPH; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+    const float u = mx == -INFINITY ? 0.f : mx, a = exp2f(m - u);
+    m = mx;
+    l *= a;
 #pragma unroll
-      for (int h = 0; h < GH; ++h) {
-        const float ah = __shfl_sync(0xffffffffu, a, h * LPH);
+    for (int r = 0; r < R; ++r) {
+      s[r] = exp2f(s[r] - u);
+      if (lane % REP == 0) l += s[r];
+    }
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[h][e] *= ah;
+    for (int h = 0; h < GH; ++h) {
+      const float ah = __shfl_sync(0xffffffffu, a, h * LPH);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int idx = h * 8 + j;
-          const float w = __shfl_sync(0xffffffffu, s[idx % R], idx / R * REP);
+      for (int e = 0; e < E; ++e) o[h][e] *= ah;
 #pragma unroll
-          for (int e = 0; e < E; ++e) o[h][e] = fmaf(w, v[j].x[e], o[h][e]);
-        }
+      for (int j = 0; j < KEYS; ++j) {
+        const int idx = h * KEYS + j;
+        const float w = __shfl_sync(0xffffffffu, s[idx % R], idx / R * REP);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[h][e] = fmaf(w, v[j].x[e], o[h][e]);
       }
     }
+    if (then.at >= 0) load_rows(v, vp + then.at);
+    now = then;
   }
 #pragma unroll
   for (int w = 1; w < LPH; w <<= 1) l += __shfl_xor_sync(0xffffffffu, l, w);
-  if (lane % LPH == 0) { s_m[warp * GH + lane / LPH] = m; s_l[warp * GH + lane / LPH] = l; }
+  if (lane % LPH == 0) { sums.m[warp][lane / LPH] = m; sums.l[warp][lane / LPH] = l; }
 #pragma unroll
   for (int h = 0; h < GH; ++h)
 #pragma unroll
-    for (int e = 0; e < E; ++e) s_o[(warp * GH + h) * DH + lane * E + e] = o[h][e];
-  finish_cta<float, DH, GH>(p, s_o, s_m, s_l, unit, split, live, b, head0, heads);
+    for (int e = 0; e < E; ++e) sums.o[warp][h][lane * E + e] = o[h][e];
 }
 
-// The splits of a unit as one, a head per CTA and a column per thread.
-template <typename T, int DH>
-__global__ void __launch_bounds__(DH) paged_join_kernel(const PagedParams p, int heads_unit) {
-  const int unit = blockIdx.x / heads_unit, h = blockIdx.x % heads_unit, d = threadIdx.x;
-  const int part = unit % p.units_h, kvh = unit / p.units_h % p.Hk, b = unit / p.units_h / p.Hk;
+
+template <typename T, int DH, int HEADS>
+__device__ __forceinline__ void attend(const PagedParams& p, const Piece& c, Sums<DH, HEADS>& sums) {
+  if constexpr (sizeof(T) == 2) attend_bf16<DH, HEADS / 8>(p, c, sums);
+  else attend_f32<DH, HEADS>(p, c, sums);
+}
+
+// CTAs that fit an SM, as the kernels' registers allow.
+template <typename T, int HEADS>
+constexpr int ctas_per_sm() { return sizeof(T) == 2 ? (HEADS == 8 ? 3 : 2) : HEADS <= 2 ? 4 : HEADS == 4 ? 3 : 2; }
+
+// Every CTA a share.
+template <typename T, int DH, int HEADS>
+__global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_attn_kernel(const PagedParams p) {
+  __shared__ Sums<DH, HEADS> sums;
   griddep_wait();
   griddep_launch();
-  const int live = splits_of(p, span_of(p, b).items);
-  if (live <= 1 || part * heads_unit + h >= p.G) return;
-  const size_t at0 = (size_t)unit * p.nsplit * heads_unit + h;
-  float m = -INFINITY;
-  for (int s = 0; s < live; ++s) m = fmaxf(m, p.part_ml[2 * (at0 + (size_t)s * heads_unit)]);
-  const float u = m == -INFINITY ? 0.f : m;
-  float l = 0.f, o = 0.f;
-#pragma unroll 4
-  for (int s = 0; s < live; ++s) {
-    const size_t at = at0 + (size_t)s * heads_unit;
-    const float f = exp2f(p.part_ml[2 * at] - u);
-    l += p.part_ml[2 * at + 1] * f;
-    o += p.part_o[at * DH + d] * f;
+  const Share sh = share_of(p);
+  const long long uh = (long long)p.Hk * p.units_h;
+  // sequences without anything to look at
+  for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
+    if (span_of(p, b).items) continue;
+    for (int i = threadIdx.x; i < p.H * DH; i += PA_WARPS * 32) store_out<T>(p, (size_t)b * p.H + i / DH, i % DH, DH, 0.f, -INFINITY, 0.f);
+    if (p.by_unit)
+      for (int i = threadIdx.x; i < uh; i += PA_WARPS * 32) p.meta[b * uh + i] = make_int4(0, 0, 0, 0);
   }
-  const size_t row = (size_t)b * p.H + kvh * p.G + part * heads_unit + h;
-  const float x = l > 0.f || l != l ? o / l : 0.f;
-  if constexpr (sizeof(T) == 2) reinterpret_cast<bf16*>(p.out)[row * DH + d] = __float2bfloat16_rn(x);
-  else reinterpret_cast<float*>(p.out)[row * DH + d] = x;
-  if (d == 0 && p.lse) p.lse[row] = (m + log2f(l)) * kLn2;
+  bool left = !p.by_unit;                                                // this CTA's join is still to be said
+  Piece c;
+  c.b = sh.b;
+  long long off = sh.off;
+  for (long long at = sh.begin; at < sh.end;) {
+    c.sp = span_of(p, c.b);
+    if (off >= c.sp.items * uh) {                                        // (the next one that has items)
+      ++c.b;
+      off = 0;
+      continue;
+    }
+    const int items = c.sp.items;
+    const int u = off >> 32 ? (int)(off / items) : (int)((unsigned)off / (unsigned)items);
+    c.item0 = (int)(off - (long long)u * items);
+    const int n = (int)min((long long)(items - c.item0), sh.end - at);
+    c.item1 = c.item0 + n;
+    c.kvh = u / p.units_h;
+    const int part = u - c.kvh * p.units_h, unit = (int)(c.b * uh) + u;
+    c.head0 = c.kvh * p.G + part * HEADS;
+    c.heads = min(HEADS, p.G - part * HEADS);
+    const int slot = 2 * (int)blockIdx.x + (at != sh.begin);             // where a part goes: a CTA has two at most, its first piece and its last
+    // (a unit whose first part is this one: of those a CTA has one at most, the last of its pieces)
+    if (c.item0 == 0 && (p.by_unit || n < items)) {
+      if (threadIdx.x == 0)
+        p.meta[p.by_unit ? unit : blockIdx.x] = make_int4(unit, slot, n == items ? 1 : (int)((at + items - 1) / sh.size - blockIdx.x) + 1, 0);
+      left = false;
+    }
+    attend<T, DH, HEADS>(p, c, sums);
+    __syncthreads();
+    for (int i = threadIdx.x; i < c.heads * DH; i += PA_WARPS * 32) {
+      const int h = i / DH, d = i % DH;
+      float m, l;
+      const float o = merge_warps(sums, h, d, m, l);
+      if (n < items) {
+        const size_t to = (size_t)slot * HEADS + h;
+        p.part_o[to * DH + d] = o;
+        if (d == 0) { p.part_ml[2 * to] = m; p.part_ml[2 * to + 1] = l; }
+      } else {
+        store_out<T>(p, (size_t)c.b * p.H + c.head0 + h, d, DH, o, m, l);
+      }
+    }
+    __syncthreads();
+    at += n;
+    off += n;
+  }
+  if (left && threadIdx.x == 0) p.meta[blockIdx.x] = make_int4(0, 0, 0, 0);
 }
 
-// How a call is cut up: heads of a unit, units of a KV head, splits and the pages of one.
+// Every unit a cluster, which meets in its CTAs' shared memory: each CTA joins a part of the outputs, sent to it by all.
+template <typename T, int DH, int HEADS>
+__global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_attn_cluster_kernel(const PagedParams p) {
+  __shared__ Sums<DH, HEADS> sums;
+  __shared__ alignas(16) float s_o[HEADS * DH];                          // [CTA][its part of the outputs]
+  __shared__ alignas(16) float2 s_ml[PA_CLUSTER][HEADS];
+  const int n = p.together, rank = blockIdx.x % n, unit = blockIdx.x / n;
+  cluster_start_arrive();
+  const int part = unit % p.units_h;
+  Piece c;
+  c.kvh = unit / p.units_h % p.Hk;
+  c.b = unit / p.units_h / p.Hk;
+  c.head0 = c.kvh * p.G + part * HEADS;
+  c.heads = min(HEADS, p.G - part * HEADS);
+  griddep_wait();
+  griddep_launch();
+  c.sp = span_of(p, c.b);
+  const int per = (c.sp.items + n - 1) / n, own = HEADS * DH / n;
+  c.item0 = min(c.sp.items, rank * per);
+  c.item1 = min(c.sp.items, c.item0 + per);
+  attend<T, DH, HEADS>(p, c, sums);
+  __syncthreads();
+  cluster_start_wait();                                                  // every CTA of the cluster runs
+  for (int i = threadIdx.x; i < c.heads * DH; i += PA_WARPS * 32) {
+    float m, l;
+    const float o = merge_warps(sums, i / DH, i % DH, m, l);
+    const int to = i / own;
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa_u32(smem_u32(&s_o[rank * own + i - to * own]), to)), "f"(o) : "memory");
+    // (the maximum and the sum of a head: to all, one each from the threads of its first columns)
+    if (i % DH < n)
+      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(mapa_u32(smem_u32(&s_ml[rank][i / DH]), i % DH)), "f"(m), "f"(l) : "memory");
+  }
+  cluster_start_arrive();
+  cluster_start_wait();                                                  // ... and has sent its sums
+  for (int j = threadIdx.x; j < own; j += PA_WARPS * 32) {
+    const int i = rank * own + j, h = i / DH;
+    if (h >= c.heads) break;
+    float m = -INFINITY, l = 0.f, o = 0.f;
+    for (int r = 0; r < n; ++r) m = fmaxf(m, s_ml[r][h].x);
+    const float u = m == -INFINITY ? 0.f : m;
+    for (int r = 0; r < n; ++r) {
+      const float f = exp2f(s_ml[r][h].x - u);
+      l += s_ml[r][h].y * f;
+      o += s_o[r * own + j] * f;
+    }
+    store_out<T>(p, (size_t)c.b * p.H + c.head0 + h, i % DH, DH, o, m, l);
+  }
+}
+
+// The parts of a unit as one.  A warp takes a head (heads_y of them per CTA) and every groups-th part.
+template <typename T, int DH>
+__global__ void __launch_bounds__(1024) paged_join_kernel(const PagedParams p, int heads_unit, int heads_y) {
+  constexpr int E = DH / 32;
+  struct alignas(4 * E) Cols {
+    float x[E];
+  };
+  __shared__ Cols s_o[32][32];
+  __shared__ float s_m[32], s_l[32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, groups = blockDim.x / 32 / heads_y, grp = warp / heads_y;
+  const int h = blockIdx.y * heads_y + warp % heads_y;
+  griddep_wait();
+  griddep_launch();
+  const int4 j = p.meta[blockIdx.x];
+  if (j.z <= 1) return;
+  const int unit = j.x, part = unit % p.units_h, kvh = unit / p.units_h % p.Hk, b = unit / p.units_h / p.Hk;
+  const bool live = part * heads_unit + h < p.G;
+  float m = -INFINITY, l = 0.f;
+  Cols o;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o.x[e] = 0.f;
+  // (the first may be the second part of its CTA, the others are the first ones of the CTAs that follow)
+#pragma unroll 8
+  for (int i = live ? grp : j.z; i < j.z; i += groups) {
+    const size_t at = (size_t)(i ? (j.y & ~1) + 2 * i : j.y) * heads_unit + h;
+    const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * at);
+    const Cols x = *reinterpret_cast<const Cols*>(p.part_o + at * DH + lane * E);
+    const float mx = fmaxf(m, ml.x), u = mx == -INFINITY ? 0.f : mx;
+    const float f = exp2f(m - u), g = exp2f(ml.x - u);
+    l = l * f + ml.y * g;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o.x[e] = o.x[e] * f + x.x[e] * g;
+    m = mx;
+  }
+  if (groups > 1) {
+    s_o[warp][lane] = o;
+    if (lane == 0) { s_m[warp] = m; s_l[warp] = l; }
+    __syncthreads();
+    if (grp) return;
+    for (int i = 1; i < groups; ++i) m = fmaxf(m, s_m[warp + i * heads_y]);
+    const float u = m == -INFINITY ? 0.f : m;
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o.x[e] = 0.f;
+    for (int i = 0; i < groups; ++i) {
+      const int w = warp + i * heads_y;
+      const float f = exp2f(s_m[w] - u);
+      l += s_l[w] * f;
+      const Cols x = s_o[w][lane];
+#pragma unroll
+      for (int e = 0; e < E; ++e) o.x[e] += x.x[e] * f;
+    }
+  }
+  if (!live) return;
+  const size_t row = (size_t)b * p.H + kvh * p.G + part * heads_unit + h;
+#pragma unroll
+  for (int e = 0; e < E; ++e) store_out<T>(p, row, lane * E + e, DH, o.x[e], m, l);
+}
+
+// How a call is cut up: heads of a unit, units of a KV head, CTAs (and of them in a cluster, 0: shares and a join).
 struct PagedPlan {
-  int heads_unit, units_h, nsplit, chunk;
+  int heads_unit, units_h, ctas, min_share, joins, together;
   long long units;
 };
-int plan_paged(int dtype, int B, int H, int Hk, int head_dim, int max_items, PagedPlan* g) {
+#ifndef MINSHARE
+#define MINSHARE 8
+#define TOGETHER_ITEMS 8
+#endif
+// max_items: pages that a sequence can have to be looked at (a window may begin and end inside one)
+int plan_paged(int dtype, int B, int H, int Hk, int head_dim, int max_len, int window, int max_sel, PagedPlan* g) {
   if (dtype != CERB_F32 && dtype != CERB_BF16) return CERB_E_ARG;
-  if (B < 0 || H < 1 || Hk < 1 || H % Hk || (head_dim != 64 && head_dim != 128) || max_items < 1) return CERB_E_SHAPE;
+  if (B < 0 || H < 1 || Hk < 1 || H % Hk || (head_dim != 64 && head_dim != 128)) return CERB_E_SHAPE;
+  const long long whole = ((long long)max_len + CERB_PAGE - 1) / CERB_PAGE, in_window = ((long long)window + 2 * CERB_PAGE - 2) / CERB_PAGE;
+  const long long items = max_sel > 0 ? max_sel : window > 0 && in_window < whole ? in_window : whole;
   const int G = H / Hk;
-  g->heads_unit = dtype == CERB_BF16 ? (G > 8 ? 16 : 8) : G > 4 ? 8 : G > 2 ? 4 : G;
+  const bool bf = dtype == CERB_BF16;
+  g->heads_unit = bf ? (G > 8 ? 16 : 8) : G > 4 ? 8 : G > 2 ? 4 : G;
   g->units_h = (G + g->heads_unit - 1) / g->heads_unit;
   g->units = (long long)B * Hk * g->units_h;
-  // splits: enough CTAs for every SM several times over, of no less than 16 pages
-  long long want = g->units ? (148 * 16 + g->units - 1) / g->units : 1;
-  int chunk = (int)((max_items + want - 1) / want);
-  chunk = (chunk + PA_WARPS - 1) / PA_WARPS * PA_WARPS;
-  if (chunk < 16) chunk = 16;
-  g->chunk = chunk;
-  g->nsplit = (max_items + chunk - 1) / chunk;
-  if (g->units * g->nsplit > 0x7fffffffll || g->units * g->heads_unit > 0x7fffffffll) return CERB_E_SHAPE;
+  if (g->units * std::max(g->heads_unit, PA_CLUSTER) > 0x7fffffffll) return CERB_E_SHAPE;
+  const int at_once = 148 * (bf ? (g->heads_unit == 8 ? ctas_per_sm<bf16, 8>() : ctas_per_sm<bf16, 16>())
+                                : g->heads_unit == 8 ? ctas_per_sm<float, 8>() : g->heads_unit == 4 ? ctas_per_sm<float, 4>() : ctas_per_sm<float, 2>());
+  g->together = 0;
+  if (g->units * items <= (long long)at_once * PA_WARPS * TOGETHER_ITEMS) {
+    g->together = 1;
+    while (g->together < PA_CLUSTER && g->units * g->together * 2 <= at_once && g->together * 2 * PA_WARPS <= items + PA_WARPS) g->together *= 2;
+    if (items > (long long)g->together * PA_WARPS * 4 * TOGETHER_ITEMS) g->together = 0;
+  }
+  g->min_share = MINSHARE;
+  if (g->together) {
+    g->ctas = (int)g->units * g->together;
+    g->joins = 0;
+    return CERB_OK;
+  }
+  const long long most = std::max(1ll, (g->units * items + g->min_share - 1) / g->min_share);
+  g->ctas = (int)std::min((long long)at_once, most);
+  g->joins = (int)std::min(g->units, (long long)g->ctas);
   return CERB_OK;
 }
-// Pages that a sequence can have to be looked at: a window may begin and end inside one.
-int max_items(int max_len, int window, int max_sel) {
-  if (max_sel > 0) return max_sel;
-  const int whole = (int)(((long long)max_len + CERB_PAGE - 1) / CERB_PAGE);
-  const long long part = ((long long)window + 2 * CERB_PAGE - 2) / CERB_PAGE;
-  return window > 0 && part < whole ? (int)part : whole;
+size_t meta_bytes(const PagedPlan& g) { return ((size_t)g.joins * sizeof(int4) + 255) & ~(size_t)255; }
+size_t part_ml_bytes(const PagedPlan& g) { return ((size_t)2 * g.ctas * g.heads_unit * 2 * sizeof(float) + 255) & ~(size_t)255; }
+size_t scratch_bytes(const PagedPlan& g, int head_dim) {
+  return g.units && !g.together ? meta_bytes(g) + part_ml_bytes(g) + (size_t)2 * g.ctas * g.heads_unit * head_dim * sizeof(float) : 0;
 }
-size_t part_ml_bytes(const PagedPlan& g) { return ((size_t)g.units * g.nsplit * g.heads_unit * 2 * sizeof(float) + 255) & ~(size_t)255; }
+
+template <typename T, int DH, int HEADS>
+cudaError_t launch(const PagedPlan& g, const PagedParams& p, cudaStream_t st) {
+  const dim3 block(PA_WARPS * 32);
+  if (g.together) return launch_pdl_cluster(paged_attn_cluster_kernel<T, DH, HEADS>, dim3((unsigned)g.ctas), block, 0, st, (unsigned)g.together, p);
+  const cudaError_t rc = launch_pdl(paged_attn_kernel<T, DH, HEADS>, dim3((unsigned)g.ctas), block, 0, st, p);
+  if (rc != cudaSuccess || g.ctas == 1) return rc;
+  // as many CTAs as run at once, of as many warps as there are parts to a unit
+  int y = 1, groups = 1;
+  while (y < HEADS && g.joins * y * 2 <= 2 * 148) y *= 2;
+  const int heads_y = HEADS / y;
+  while (2 * groups * heads_y <= 32 && groups * g.joins < g.ctas) groups *= 2;
+  return launch_pdl(paged_join_kernel<T, DH>, dim3((unsigned)g.joins, (unsigned)y), dim3((unsigned)(32 * heads_y * groups)), 0, st, p, HEADS, heads_y);
+}
 
 }  // namespace
 
@@ -488,8 +765,8 @@ int cerb_paged_attention_scratch_bytes(int32_t dtype, int32_t B, int32_t n_heads
                                        int32_t max_sel, size_t* bytes_out) {
   if (!bytes_out || max_len < 1 || window < 0 || max_sel < 0) return CERB_E_ARG;
   PagedPlan g;
-  CERB_TRY(plan_paged(dtype, B, n_heads, n_kv_heads, head_dim, max_items(max_len, window, max_sel), &g));
-  *bytes_out = g.nsplit > 1 ? part_ml_bytes(g) + (size_t)g.units * g.nsplit * g.heads_unit * head_dim * sizeof(float) : 0;
+  CERB_TRY(plan_paged(dtype, B, n_heads, n_kv_heads, head_dim, max_len, window, max_sel, &g));
+  *bytes_out = scratch_bytes(g, head_dim);
   return CERB_OK;
 }
 
@@ -499,12 +776,11 @@ int cerb_paged_attention(const cerb_paged_attn_args* a, void* stream) {
   if (a->max_pages < 1 || a->max_pages > (1 << 26) || a->n_pool_pages < 1 || a->max_len < 1 || a->window < 0 || (a->sel && a->max_sel < 1)) return CERB_E_ARG;
   const int max_sel = a->sel ? a->max_sel : 0;
   PagedPlan g;
-  CERB_TRY(plan_paged(a->dtype, a->B, a->n_heads, a->n_kv_heads, a->head_dim, max_items(a->max_len, a->window, max_sel), &g));
+  CERB_TRY(plan_paged(a->dtype, a->B, a->n_heads, a->n_kv_heads, a->head_dim, a->max_len, a->window, max_sel, &g));
   const int es = a->dtype == CERB_BF16 ? 2 : 4;
   if (a->q_row_stride * es % 16 || a->q_head_stride * es % 16) return CERB_E_ARG;
   if (((uintptr_t)a->q | (uintptr_t)a->k_pool | (uintptr_t)a->v_pool | (uintptr_t)a->scratch) & 15) return CERB_E_ARG;
-  size_t need = 0;
-  CERB_TRY(cerb_paged_attention_scratch_bytes(a->dtype, a->B, a->n_heads, a->n_kv_heads, a->head_dim, a->max_len, a->window, max_sel, &need));
+  const size_t need = scratch_bytes(g, a->head_dim);
   if (need > a->scratch_bytes || (need && !a->scratch)) return CERB_E_NOMEM;
   if (a->B == 0) return CERB_OK;
   PagedParams p;
@@ -518,8 +794,10 @@ int cerb_paged_attention(const cerb_paged_attn_args* a, void* stream) {
   p.n_sel = a->n_sel;
   p.out = a->out;
   p.lse = a->lse;
-  p.part_ml = (float*)a->scratch;
-  p.part_o = (float*)((char*)a->scratch + part_ml_bytes(g));
+  p.meta = (int4*)a->scratch;
+  p.by_unit = g.units <= g.ctas;
+  p.part_ml = (float*)((char*)a->scratch + meta_bytes(g));
+  p.part_o = (float*)((char*)p.part_ml + part_ml_bytes(g));
   p.q_row = a->q_row_stride;
   p.q_head = a->q_head_stride;
   p.B = a->B;
@@ -531,28 +809,22 @@ int cerb_paged_attention(const cerb_paged_attn_args* a, void* stream) {
   p.n_pool_pages = a->n_pool_pages;
   p.max_sel = a->max_sel;
   p.window = a->window;
-  p.nsplit = g.nsplit;
-  p.chunk = g.chunk;
+  p.min_share = g.min_share;
+  p.together = g.together;
   p.scale_log2 = a->scale * kLog2e;
   cudaStream_t st = (cudaStream_t)stream;
-  void (*kern)(const PagedParams);
   const bool wide = a->head_dim == 128;
+  cudaError_t rc;
   if (a->dtype == CERB_BF16)
-    kern = g.heads_unit == 16 ? (wide ? paged_attn_bf16_kernel<128, 2> : paged_attn_bf16_kernel<64, 2>)
-                              : (wide ? paged_attn_bf16_kernel<128, 1> : paged_attn_bf16_kernel<64, 1>);
+    rc = g.heads_unit == 16 ? (wide ? launch<bf16, 128, 16>(g, p, st) : launch<bf16, 64, 16>(g, p, st))
+                            : (wide ? launch<bf16, 128, 8>(g, p, st) : launch<bf16, 64, 8>(g, p, st));
   else
     switch (g.heads_unit) {
-      case 1: kern = wide ? paged_attn_f32_kernel<128, 1> : paged_attn_f32_kernel<64, 1>; break;
-      case 2: kern = wide ? paged_attn_f32_kernel<128, 2> : paged_attn_f32_kernel<64, 2>; break;
-      case 4: kern = wide ? paged_attn_f32_kernel<128, 4> : paged_attn_f32_kernel<64, 4>; break;
-      default: kern = wide ? paged_attn_f32_kernel<128, 8> : paged_attn_f32_kernel<64, 8>;
+      case 1: rc = wide ? launch<float, 128, 1>(g, p, st) : launch<float, 64, 1>(g, p, st); break;
+      case 2: rc = wide ? launch<float, 128, 2>(g, p, st) : launch<float, 64, 2>(g, p, st); break;
+      case 4: rc = wide ? launch<float, 128, 4>(g, p, st) : launch<float, 64, 4>(g, p, st); break;
+      default: rc = wide ? launch<float, 128, 8>(g, p, st) : launch<float, 64, 8>(g, p, st);
     }
-  if (launch_pdl(kern, dim3((unsigned)(g.units * g.nsplit)), dim3(PA_WARPS * 32), 0, st, p) != cudaSuccess) return CERB_E_CUDA;
-  if (g.nsplit == 1) return CERB_OK;
-  const dim3 grid((unsigned)(g.units * g.heads_unit)), block((unsigned)a->head_dim);
-  cudaError_t rc;
-  if (a->dtype == CERB_BF16) rc = launch_pdl(wide ? paged_join_kernel<bf16, 128> : paged_join_kernel<bf16, 64>, grid, block, 0, st, p, g.heads_unit);
-  else rc = launch_pdl(wide ? paged_join_kernel<float, 128> : paged_join_kernel<float, 64>, grid, block, 0, st, p, g.heads_unit);
   return rc == cudaSuccess ? CERB_OK : CERB_E_CUDA;
 }
 

@@ -289,12 +289,13 @@ def test_pages_outside_the_pool_hold_no_keys(dtype):
 def test_attention_scratch_and_output_without_lse():
     c = Cache([3000, 70], 2, 128, "bf16", 41)
     _, gq = c.queries(8, 6)
-    a, lse = binding.paged_attention(gq, *c.gpu, c.glens, 0.1, 3000)
+    # (a cache that may be long enough for shares and a join: those need the scratch)
+    a, lse = binding.paged_attention(gq, *c.gpu, c.glens, 0.1, 60000)
     scratch = torch.full((1 << 22,), 255, dtype=torch.uint8, device="cuda")
-    b, none = binding.paged_attention(gq, *c.gpu, c.glens, 0.1, 3000, want_lse=False, scratch=scratch)
+    b, none = binding.paged_attention(gq, *c.gpu, c.glens, 0.1, 60000, want_lse=False, scratch=scratch)
     assert none is None and torch.equal(a, b)
     with pytest.raises(binding.CerbError) as e:
-        binding.paged_attention(gq, *c.gpu, c.glens, 0.1, 3000, scratch=scratch[:64])
+        binding.paged_attention(gq, *c.gpu, c.glens, 0.1, 60000, scratch=scratch[:64])
     assert e.value.code == binding.E_NOMEM
 
 
