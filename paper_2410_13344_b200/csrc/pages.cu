@@ -1,16 +1,18 @@
 // Bookkeeping of a paged KV cache, and the append into it.
 #include <string.h>
 
+#include <algorithm>
+
 #include "cerb_internal.cuh"
 
 namespace cerb {
 
 namespace {
 
-constexpr int PLAN_THREADS = 1024;
-constexpr int PLAN_CLUSTER = 8;
-// Up to this many rows one CTA fills them; more are spread over a cluster.
-constexpr int kPlanRowsOneCta = 8192;
+constexpr int PLAN_THREADS = 1024, PLAN_FEW = 256;
+constexpr int TRIM_CLUSTER = 8;
+// Up to this many rows one CTA fills them; more are spread over the SMs, and a second launch changes the state.
+constexpr int kPlanRowsAlone = 4096;
 constexpr int kMaxRequests = 8192;      // four words each of a CTA's shared memory
 
 struct PagesParams {
@@ -26,8 +28,9 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 __device__ __forceinline__ int pages_of(int tokens) { return (int)(((unsigned)tokens + CERB_PAGE - 1) / CERB_PAGE); }
 
 // Inclusive sum over the CTA's threads; `total` is that of all.
-template <typename T>
+template <int THREADS, typename T>
 __device__ __forceinline__ T block_scan(T v, T* red, T& total) {
+  constexpr int WARPS = THREADS / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -36,13 +39,13 @@ __device__ __forceinline__ T block_scan(T v, T* red, T& total) {
   }
   if (lane == 31) red[warp] = v;
   __syncthreads();
-  T w = red[lane];
+  T w = lane < WARPS ? red[lane] : 0;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
+  for (int o = 1; o < WARPS; o <<= 1) {
     const T u = __shfl_up_sync(0xffffffffu, w, o);
     if (lane >= o) w += u;
   }
-  total = __shfl_sync(0xffffffffu, w, 31);
+  total = __shfl_sync(0xffffffffu, w, WARPS - 1);
   const T before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
   __syncthreads();
   return v + (warp ? before : 0);
@@ -63,31 +66,32 @@ __device__ __forceinline__ int find_request(const int* ends, int B, int i) {
 }
 
 // Two prefix sums over the requests (rows, and pages of those that fit) and then a row per element: its request, position and slot.
-// A launch and nothing else: every CTA of the cluster sums up for itself, and lengths and free count change behind the cluster's
-// barrier, when all have read them.  New pages never lie where a row of this call finds an old one, so the table may change before.
-template <bool CLUSTER>
-__global__ void __launch_bounds__(PLAN_THREADS, 1) pages_plan_kernel(const PagesParams p) {
+// New pages never lie where a row of this call finds an old one, so the table may change at once.  Lengths and free count change when all have read them:
+// with one CTA (ALONE) at its end, with more (each of which sums up for itself) in a launch of their own.
+template <int THREADS, bool ALONE>
+__global__ void __launch_bounds__(THREADS, 1) pages_plan_kernel(const PagesParams p) {
   extern __shared__ __align__(16) int sm[];
   int *ends = sm, *lens = ends + p.B, *base = lens + p.B, *give = base + p.B;     // rows before and of b, length, new pages before, 1 if granted
   __shared__ long long red_rows[32];
-  __shared__ int red_pages[32];
+  __shared__ int red_pages[32], s_taken;
   const int tid = threadIdx.x;
-  const unsigned cta = CLUSTER ? blockIdx.x : 0, ctas = CLUSTER ? PLAN_CLUSTER : 1;
+  const unsigned cta = ALONE ? 0 : blockIdx.x, ctas = ALONE ? 1 : gridDim.x;
+  if (tid == 0) s_taken = 0;
   griddep_wait();
   griddep_launch();
   const int n_free = min(max(*p.n_free, 0), p.free_cap);
   long long rows_before = 0;
-  int pages_before = 0, taken = 0;
-  for (int b0 = 0; b0 < p.B; b0 += PLAN_THREADS) {
+  int pages_before = 0;
+  for (int b0 = 0; b0 < p.B; b0 += THREADS) {
     const int b = b0 + tid;
     const bool live = b < p.B;
     const int len = live ? held_tokens(p, b) : 0, n = live ? max(p.n_new[b], 0) : 0;
     long long rows_total;
-    const long long end = rows_before + block_scan((long long)n, red_rows, rows_total);
+    const long long end = rows_before + block_scan<THREADS>((long long)n, red_rows, rows_total);
     const bool fits = live && (long long)len + n <= (long long)p.max_pages * CERB_PAGE && end <= p.rows;
     const int need = fits ? pages_of(len + n) - pages_of(len) : 0;
     int pages_total;
-    const int cum = pages_before + block_scan(need, red_pages, pages_total);
+    const int cum = pages_before + block_scan<THREADS>(need, red_pages, pages_total);
     const bool ok = fits && (need == 0 || cum <= n_free);
     if (live) {
       ends[b] = (int)min(end, 0x7fffffffll);
@@ -97,42 +101,45 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) pages_plan_kernel(const Pages
       if (cta == 0) {
         p.granted[b] = ok ? n : 0;
         p.row_off[b + 1] = (int)min(end, 0x7fffffffll);
+        // (the ones with new pages that get them are the first ones)
+        if (ALONE && ok && need) atomicMax(&s_taken, cum);
       }
     }
-    // (the ones with new pages that get them are the first ones)
-    int t;
-    block_scan(ok ? need : 0, red_pages, t);
-    taken += t;
     rows_before += rows_total;
     pages_before += pages_total;
   }
   if (cta == 0 && tid == 0) p.row_off[0] = 0;
-  if (CLUSTER) cluster_arrive();
   __syncthreads();
   const int total = (int)min(rows_before, (long long)p.rows);
   const bool wide = !(((uintptr_t)p.slot | (uintptr_t)p.pos | (uintptr_t)p.seq) & 15);
-  for (int r0 = 4 * (int)(cta * PLAN_THREADS + tid); r0 < p.rows; r0 += 4 * (int)(ctas * PLAN_THREADS)) {
+  for (int r0 = 4 * (int)(cta * THREADS + tid); r0 < p.rows; r0 += 4 * (int)(ctas * THREADS)) {
     int slot[4], pos[4], seq[4];
+    const int32_t* from[4];
+    int32_t* entry[4];
     int b = r0 < total ? find_request(ends, p.B, r0) : 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r = r0 + i;
       slot[i] = pos[i] = seq[i] = -1;
+      from[i] = nullptr;
+      entry[i] = nullptr;
       if (r >= total) continue;
       while (ends[b] <= r) ++b;
       if (!give[b]) continue;
       const int first = b ? ends[b - 1] : 0, len = lens[b], at = len + r - first, j = at / CERB_PAGE, held = pages_of(len);
-      int32_t* entry = p.page_table + (size_t)b * p.max_pages + j;
-      int page;
-      if (j < held) {
-        page = *entry;
-      } else {
-        page = p.free_pages[n_free - 1 - base[b] - (j - held)];
-        if (at % CERB_PAGE == 0) *entry = page;
-      }
-      slot[i] = page * CERB_PAGE + at % CERB_PAGE;
+      int32_t* e = p.page_table + (size_t)b * p.max_pages + j;
+      from[i] = j < held ? e : p.free_pages + (n_free - 1 - base[b] - (j - held));
+      if (j >= held && at % CERB_PAGE == 0) entry[i] = e;
       pos[i] = at;
       seq[i] = b;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (from[i]) slot[i] = *from[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (entry[i]) *entry[i] = slot[i];
+      if (from[i]) slot[i] = slot[i] * CERB_PAGE + pos[i] % CERB_PAGE;
     }
     if (wide && r0 + 3 < p.rows) {
       *reinterpret_cast<int4*>(p.slot + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
@@ -144,15 +151,29 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) pages_plan_kernel(const Pages
         if (r0 + i < p.rows) { p.slot[r0 + i] = slot[i]; p.pos[r0 + i] = pos[i]; p.seq[r0 + i] = seq[i]; }
     }
   }
-  if (CLUSTER) cluster_wait();
-  if (cta != 0) return;
-  for (int b = tid; b < p.B; b += PLAN_THREADS)
+  if (!ALONE) return;
+  for (int b = tid; b < p.B; b += THREADS)
     if (give[b]) p.len[b] = lens[b] + ends[b] - (b ? ends[b - 1] : 0);
-  if (tid == 0) *p.n_free = n_free - taken;
+  if (tid == 0) *p.n_free = n_free - s_taken;
+}
+
+__global__ void __launch_bounds__(PLAN_THREADS, 1) pages_grant_kernel(const PagesParams p) {
+  __shared__ int red_pages[32];
+  griddep_wait();
+  griddep_launch();
+  int taken = 0;
+  for (int b = threadIdx.x; b < p.B; b += PLAN_THREADS) {
+    const int n = p.granted[b], len = held_tokens(p, b);
+    taken += pages_of(len + n) - pages_of(len);
+    if (n) p.len[b] = len + n;
+  }
+  int total;
+  block_scan<PLAN_THREADS>(taken, red_pages, total);
+  if (threadIdx.x == 0) *p.n_free = min(max(*p.n_free, 0), p.free_cap) - total;
 }
 
 // Pages behind the lengths to keep go back to the list, the last one of the last request first: a trim to the lengths before a
-// plan leaves the list as it was.
+// plan leaves the list as it was.  One cluster: lengths and free count change behind its barrier.
 __global__ void __launch_bounds__(PLAN_THREADS, 1) pages_trim_kernel(const PagesParams p) {
   extern __shared__ __align__(16) int sm[];
   int *ends = sm, *news = ends + p.B;                          // pages given back before and of b; the length kept
@@ -167,18 +188,32 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) pages_trim_kernel(const Pages
     const int b = b0 + tid;
     const int len = b < p.B ? held_tokens(p, b) : 0, keep = b < p.B ? min(max(p.n_new[b], 0), len) : 0;
     int t;
-    const int end = total + block_scan(pages_of(len) - pages_of(keep), red_pages, t);
+    const int end = total + block_scan<PLAN_THREADS>(pages_of(len) - pages_of(keep), red_pages, t);
     if (b < p.B) { ends[b] = end; news[b] = keep; }
     total += t;
   }
   cluster_arrive();
   __syncthreads();
-  for (int i = (int)(cta * PLAN_THREADS + tid); i < total; i += PLAN_CLUSTER * PLAN_THREADS) {
-    const int b = find_request(ends, p.B, i);
-    int32_t* entry = p.page_table + (size_t)b * p.max_pages + pages_of(news[b]) + i - (b ? ends[b - 1] : 0);
-    const int at = n_free + total - 1 - i;
-    if (at < p.free_cap) p.free_pages[at] = *entry;
-    *entry = -1;
+  for (int i0 = 4 * (int)(cta * PLAN_THREADS + tid); i0 < total; i0 += 4 * TRIM_CLUSTER * PLAN_THREADS) {
+    int32_t* entry[4];
+    int page[4], b = find_request(ends, p.B, i0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      entry[i] = nullptr;
+      if (i0 + i >= total) continue;
+      while (ends[b] <= i0 + i) ++b;
+      entry[i] = p.page_table + (size_t)b * p.max_pages + pages_of(news[b]) + i0 + i - (b ? ends[b - 1] : 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (entry[i]) page[i] = *entry[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (entry[i]) {
+        const int at = n_free + total - 1 - i0 - i;
+        if (at < p.free_cap) p.free_pages[at] = page[i];
+        *entry[i] = -1;
+      }
   }
   cluster_wait();
   if (cta != 0) return;
@@ -221,12 +256,12 @@ __device__ __forceinline__ uint32_t upper(uint32_t a, uint32_t b, float) {
   return __float_as_uint(r);
 }
 
-// A run is what follows one another in the list within one page.  LANES threads own a run of one head, each 16 bytes of the head:
-// a run has one owner, so the page's minimum and maximum need no atomics and do not depend on any order.  All of a run's rows are
-// in flight at once.  Keys and values are for different threads (blockIdx.y).
+// A run is what follows one another in the list within one page.  LANES threads own the runs of one head that begin in a window of `block` rows of the
+// list, each 16 bytes of the head: a run has one owner, so the page's minimum and maximum need no atomics and do not depend on any
+// order.  BATCH rows are in flight at once.  Keys and values are for different threads (blockIdx.y).
 template <typename T, int DH>
-__global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams p) {
-  constexpr int LANES = DH * (int)sizeof(T) / 16, ROW = DH * (int)sizeof(T);
+__global__ void __launch_bounds__(256, 4) kv_append_kernel(const AppendParams p) {
+  constexpr int LANES = DH * (int)sizeof(T) / 16, ROW = DH * (int)sizeof(T), BATCH = CERB_PAGE / 4;
   const int lane = threadIdx.x % LANES;
   const long long item = ((long long)blockIdx.x * 256 + threadIdx.x) / LANES;
   const int h = (int)(item % p.H);
@@ -236,55 +271,64 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams p) {
   const long long row = values ? p.v_row : p.k_row;
   char* pool = (values ? p.v_pool : p.k_pool) + lane * 16;
   const bool sums = !values && p.k_min != nullptr;
+  const unsigned group = LANES == 32 ? 0xffffffffu : ((1u << LANES) - 1) << ((threadIdx.x & 31) / LANES * LANES);
   griddep_wait();
   griddep_launch();
-  for (long long t = t0; t < min((long long)p.T, t0 + p.block); ++t) {
-    const int s0 = p.slot[t];
-    if (s0 < 0 || s0 >= p.n_slots) continue;
-    const int page = s0 / CERB_PAGE;
-    if (t > 0) {
-      const int before = p.slot[t - 1];
-      if (before >= 0 && before / CERB_PAGE == page) continue;           // its owner is that one's
-    }
-    uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+  auto page_of = [&](long long t) {
+    const int s = t >= 0 && t < p.T ? p.slot[t] : -1;
+    return s >= 0 && s < p.n_slots ? s / CERB_PAGE : -1;
+  };
+  // which rows of the window begin a run
+  unsigned starts = 0;
+#pragma unroll
+  for (int w = 0; w < CERB_PAGE; w += LANES) {
+    const long long t = t0 + w + lane;
+    const int page = w + lane < p.block ? page_of(t) : -1;
+    const unsigned mine = __ballot_sync(group, page >= 0 && page_of(t - 1) != page) >> ((threadIdx.x & 31) / LANES * LANES);
+    starts |= (LANES == 32 ? mine : mine & ((1u << LANES) - 1)) << w;
+  }
+  for (; starts; starts &= starts - 1) {
+    const long long t = t0 + __ffs(starts) - 1;
+    const int page = p.slot[t] / CERB_PAGE;
+    uint4 lo = make_uint4(0, 0, 0, 0), hi = lo, old_lo = lo, old_hi = lo;
     bool fresh = false, first = true;
-    char* at = sums ? p.k_min + ((size_t)page * p.H + h) * ROW + lane * 16 : nullptr;
-    char* at_hi = sums ? p.k_max + ((size_t)page * p.H + h) * ROW + lane * 16 : nullptr;
-    // (a run is at most a page long if no slot comes twice)
-    for (long long u = t;; u += CERB_PAGE) {
-      int off[CERB_PAGE];
-      uint4 x[CERB_PAGE];
+    uint4* at = reinterpret_cast<uint4*>(sums ? p.k_min + ((size_t)page * p.H + h) * ROW + lane * 16 : nullptr);
+    uint4* at_hi = reinterpret_cast<uint4*>(sums ? p.k_max + ((size_t)page * p.H + h) * ROW + lane * 16 : nullptr);
+    if (sums) { old_lo = *at; old_hi = *at_hi; }
+    char* to = pool + ((size_t)page * p.H + h) * CERB_PAGE * ROW;
+    auto take = [&](const uint4& x, const uint4& y) {
+      if (first) { lo = x; hi = y; first = false; return; }
+      lo = make_uint4(lower(lo.x, x.x, T()), lower(lo.y, x.y, T()), lower(lo.z, x.z, T()), lower(lo.w, x.w, T()));
+      hi = make_uint4(upper(hi.x, y.x, T()), upper(hi.y, y.y, T()), upper(hi.z, y.z, T()), upper(hi.w, y.w, T()));
+    };
+    for (long long u = t;; u += BATCH) {
+      int off[BATCH];
+      uint4 x[BATCH];
       int n = 0;
 #pragma unroll
-      for (int i = 0; i < CERB_PAGE; ++i) {
+      for (int i = 0; i < BATCH; ++i) {
         const int s = u + i < p.T ? p.slot[u + i] : -1;
         off[i] = s >= 0 && s / CERB_PAGE == page ? s % CERB_PAGE : -1;
       }
 #pragma unroll
-      for (int i = 0; i < CERB_PAGE; ++i) {
+      for (int i = 0; i < BATCH; ++i) {
         if (n == i && off[i] >= 0) ++n;
         if (i < n) x[i] = *reinterpret_cast<const uint4*>(src + (u + i) * row);
       }
 #pragma unroll
-      for (int i = 0; i < CERB_PAGE; ++i) {
+      for (int i = 0; i < BATCH; ++i) {
         if (i >= n) continue;
-        *reinterpret_cast<uint4*>(pool + (((size_t)page * p.H + h) * CERB_PAGE + off[i]) * ROW) = x[i];
+        *reinterpret_cast<uint4*>(to + off[i] * ROW) = x[i];
         if (!sums) continue;
         fresh |= off[i] == 0;
-        if (first) { lo = hi = x[i]; first = false; continue; }
-        lo = make_uint4(lower(lo.x, x[i].x, T()), lower(lo.y, x[i].y, T()), lower(lo.z, x[i].z, T()), lower(lo.w, x[i].w, T()));
-        hi = make_uint4(upper(hi.x, x[i].x, T()), upper(hi.y, x[i].y, T()), upper(hi.z, x[i].z, T()), upper(hi.w, x[i].w, T()));
+        take(x[i], x[i]);
       }
-      if (n < CERB_PAGE) break;
+      if (n < BATCH) break;
     }
     if (!sums) continue;
-    if (!fresh) {
-      const uint4 a = *reinterpret_cast<const uint4*>(at), b = *reinterpret_cast<const uint4*>(at_hi);
-      lo = make_uint4(lower(lo.x, a.x, T()), lower(lo.y, a.y, T()), lower(lo.z, a.z, T()), lower(lo.w, a.w, T()));
-      hi = make_uint4(upper(hi.x, b.x, T()), upper(hi.y, b.y, T()), upper(hi.z, b.z, T()), upper(hi.w, b.w, T()));
-    }
-    *reinterpret_cast<uint4*>(at) = lo;
-    *reinterpret_cast<uint4*>(at_hi) = hi;
+    if (!fresh) take(old_lo, old_hi);
+    *at = lo;
+    *at_hi = hi;
   }
 }
 
@@ -331,15 +375,17 @@ int cerb_pages_plan(const cerb_pages* s, const int32_t* n_new, int32_t rows, int
   p.rows = rows;
   const size_t smem = 4 * (size_t)p.B * sizeof(int);
   cudaStream_t st = (cudaStream_t)stream;
-  if (rows <= kPlanRowsOneCta) {
-    static std::atomic<uint64_t> done{0};
-    CERB_TRY(allow_smem(pages_plan_kernel<false>, done, 4 * kMaxRequests * (int)sizeof(int)));
-    return launch_pdl(pages_plan_kernel<false>, dim3(1), dim3(PLAN_THREADS), smem, st, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
+  static std::atomic<uint64_t> done[2];
+  if (p.B <= PLAN_FEW && rows <= 4 * PLAN_FEW)
+    return launch_pdl(pages_plan_kernel<PLAN_FEW, true>, dim3(1), dim3(PLAN_FEW), smem, st, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
+  if (rows <= kPlanRowsAlone) {
+    CERB_TRY(allow_smem(pages_plan_kernel<PLAN_THREADS, true>, done[0], 4 * kMaxRequests * (int)sizeof(int)));
+    return launch_pdl(pages_plan_kernel<PLAN_THREADS, true>, dim3(1), dim3(PLAN_THREADS), smem, st, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
   }
-  static std::atomic<uint64_t> done{0};
-  CERB_TRY(allow_smem(pages_plan_kernel<true>, done, 4 * kMaxRequests * (int)sizeof(int)));
-  return launch_pdl_cluster(pages_plan_kernel<true>, dim3(PLAN_CLUSTER), dim3(PLAN_THREADS), smem, st, PLAN_CLUSTER, p) == cudaSuccess
-             ? CERB_OK : CERB_E_CUDA;
+  CERB_TRY(allow_smem(pages_plan_kernel<PLAN_THREADS, false>, done[1], 4 * kMaxRequests * (int)sizeof(int)));
+  const int ctas = std::min(148, (rows + 4 * PLAN_THREADS - 1) / (4 * PLAN_THREADS));
+  if (launch_pdl(pages_plan_kernel<PLAN_THREADS, false>, dim3((unsigned)ctas), dim3(PLAN_THREADS), smem, st, p) != cudaSuccess) return CERB_E_CUDA;
+  return launch_pdl(pages_grant_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
 }
 
 int cerb_pages_trim(const cerb_pages* s, const int32_t* keep, void* stream) {
@@ -350,8 +396,8 @@ int cerb_pages_trim(const cerb_pages* s, const int32_t* keep, void* stream) {
   p.n_new = keep;
   static std::atomic<uint64_t> done{0};
   CERB_TRY(allow_smem(pages_trim_kernel, done, 2 * kMaxRequests * (int)sizeof(int)));
-  return launch_pdl_cluster(pages_trim_kernel, dim3(PLAN_CLUSTER), dim3(PLAN_THREADS), 2 * (size_t)p.B * sizeof(int), (cudaStream_t)stream,
-                            PLAN_CLUSTER, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
+  return launch_pdl_cluster(pages_trim_kernel, dim3(TRIM_CLUSTER), dim3(PLAN_THREADS), 2 * (size_t)p.B * sizeof(int), (cudaStream_t)stream,
+                            TRIM_CLUSTER, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
 }
 
 int cerb_kv_append(const cerb_kv_append_args* a, void* stream) {
@@ -381,7 +427,7 @@ int cerb_kv_append(const cerb_kv_append_args* a, void* stream) {
   p.H = a->n_kv_heads;
   p.n_slots = (long long)a->n_pool_pages * CERB_PAGE;
   // a token to a group of threads while they all fit the GPU at once, else as many as make it fit, a page at most
-  const long long lanes = a->head_dim * es / 16, threads = 2 * (long long)p.T * p.H * lanes, room = 148ll * 2048;
+  const long long lanes = a->head_dim * es / 16, threads = 2 * (long long)p.T * p.H * lanes, room = 148ll * 512;
   p.block = (int)((threads + room - 1) / room);
   if (p.block > CERB_PAGE) p.block = CERB_PAGE;
   const long long groups = ((long long)p.T + p.block - 1) / p.block * p.H, ctas = (groups * lanes + 255) / 256;
