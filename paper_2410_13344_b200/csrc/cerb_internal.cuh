@@ -105,16 +105,24 @@ inline cudaError_t launch_pdl_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
-// Lets a kernel have `bytes` of dynamic shared memory on the current device, once per device (`done`: a bit for each of the first 64).
+// Sets an attribute of a kernel on the current device, once per device (`done`: a bit for each of the first 64).
 template <typename K>
-inline int allow_smem(K kern, std::atomic<uint64_t>& done, int bytes) {
+inline int set_attribute_once(K kern, std::atomic<uint64_t>& done, cudaFuncAttribute attribute, int value) {
   int dev = 0;
   CERB_CUDA_OK(cudaGetDevice(&dev));
   const uint64_t bit = dev < 64 ? 1ull << dev : 0;
   if (done & bit) return CERB_OK;
-  CERB_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  CERB_CUDA_OK(cudaFuncSetAttribute(kern, attribute, value));
   done |= bit;
   return CERB_OK;
+}
+template <typename K>
+inline int allow_smem(K kern, std::atomic<uint64_t>& done, int bytes) {
+  return set_attribute_once(kern, done, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+template <typename K>
+inline int allow_wide_clusters(K kern, std::atomic<uint64_t>& done) {
+  return set_attribute_once(kern, done, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
 }
 
 constexpr int kPathMax = CERB_MAX_DEPTH + 1;

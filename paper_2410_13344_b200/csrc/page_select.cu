@@ -13,25 +13,33 @@
 
 #include <algorithm>
 
-#include "cerb_internal.cuh"
+#include "paged_common.cuh"
 
 namespace cerb {
 
 namespace {
 
 constexpr int SC_WARPS = 4;
-constexpr int SEL_THREADS = 1024;
-constexpr int SEL_BINS = 1024;
+constexpr int SEL_THREADS = 512;
+constexpr int SEL_KEEP = 8192;              // scores that shared memory keeps: those of caches of up to so many pages
+constexpr int SEL_BINS = 512;
 constexpr int SEL_LIST = 1024;              // pages near the border that are ranked one against another
-constexpr int SEL_SMEM_PAGES = 40960;       // scores of up to this many pages lie in shared memory
-constexpr int kMaxSelectPages = 1 << 17;    // (bit masks of them do always)
+constexpr int kMaxSelectPages = 1 << 17;    // (a bit mask of them lies in shared memory)
+
+// What a CTA that scores pages leaves behind, over those that are up for selection.
+struct ChunkScores {
+  float bound;                 // of the error of its scores
+  float lo, hi;                // smallest and largest score
+  int odd;                     // scores that are not finite
+};
 
 struct SelectParams {
   const void *q, *k_min, *k_max;
   const int32_t *page_table, *len;
   int32_t *sel, *n_sel;
-  float *score, *bound;        // [unit][max_pages]; [unit][chunks]: the largest error bound of a chunk
-  double* again;               // [unit][max_pages]
+  float* score;                // [unit][max_pages]
+  ChunkScores* chunk;          // [unit][chunks]
+  unsigned long long* again;   // [unit][max_pages]: scores of 64 bits as ordered whole numbers
   long long q_row, q_head;     // elements
   int B, H, Hk, G, max_pages, n_pool_pages, K, n_first, n_last, chunks;
 };
@@ -56,24 +64,77 @@ __device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
 }
 __device__ __forceinline__ uint32_t abs2(uint32_t a) { return a & 0x7fff7fffu; }
 
-// How far a score may be off, relative to S = sum_d |q_d| max(|kmin_d|, |kmax_d|).
-// bf16: 2 Dh <= 256 products in steps of 16; a step of the tensor cores keeps at least 24 bits of the largest of its 17 addends, each of which is at most
-// S: 16 steps of 17 x 2^-23 S, under 2^-14 S with S's own error.  fp32: sums of Dh products in chains of at most Dh / 32 + 5 roundings: under 2^-19 S.
+// How far a score may be off, relative to S = sum_d |q_d| |k_d|, k_d the one of kmin_d and kmax_d that counts for q_d's sign.
+// bf16: q's positive and negative elements are products of their own, Dh / 16 <= 8 steps of the tensor cores each, and a step keeps at least 24 bits of the
+// largest of its 17 addends, each of which is at most the product's share of S: 8 x 17 x 2^-23 S, three more roundings and S's own error: under 2^-15.5 S.
+// fp32: chains of at most Dh / 32 + 5 roundings: under 2^-19 S.
 template <typename T> __device__ __forceinline__ float error_factor();
-template <> __device__ __forceinline__ float error_factor<bf16>() { return 1.0f / 16384; }
+template <> __device__ __forceinline__ float error_factor<bf16>() { return 2.1579186e-5f; }
 template <> __device__ __forceinline__ float error_factor<float>() { return 1.0f / 524288; }
 
+// What is known of a CTA's scores, from what its threads know.
+template <typename T>
+__device__ __forceinline__ void leave_chunk(const SelectParams& p, int unit, int chunk, float bound, float lo, float hi, bool odd) {
+  __shared__ ChunkScores s_c[SC_WARPS];
+  const int warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int w = 1; w < 32; w <<= 1) {
+    bound = fmaxf(bound, __shfl_xor_sync(0xffffffffu, bound, w));
+    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, w));
+    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, w));
+  }
+  odd = __any_sync(0xffffffffu, odd);
+  if ((threadIdx.x & 31) == 0) s_c[warp] = ChunkScores{bound, lo, hi, odd};
+  __syncthreads();
+  if (threadIdx.x) return;
+  ChunkScores c = s_c[0];
+  for (int w = 1; w < SC_WARPS; ++w) {
+    c.bound = fmaxf(c.bound, s_c[w].bound);
+    c.lo = fminf(c.lo, s_c[w].lo);
+    c.hi = fmaxf(c.hi, s_c[w].hi);
+    c.odd |= s_c[w].odd;
+  }
+  c.bound *= error_factor<T>();
+  p.chunk[(size_t)unit * p.chunks + chunk] = c;
+}
+
 // bf16 scores: 16 pages on the rows of a warp MMA, eight heads on its columns, kmax and kmin straight from global memory in the order in which the lanes
-// load them.  The bound S is a third product.
+// load them, the next 16 pages' on their way.  S is a product like the scores, of absolute values.
 template <int DH>
-__global__ void __launch_bounds__(SC_WARPS * 32) page_score_bf16_kernel(const SelectParams p) {
+__global__ void __launch_bounds__(SC_WARPS * 32, 3) page_score_bf16_kernel(const SelectParams p) {
   constexpr int KC = DH / 32, LD = DH + 8;
   extern __shared__ __align__(16) bf16 q_s[];                            // [heads padded to 8][LD]
-  __shared__ float s_e[SC_WARPS];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int chunk = blockIdx.x % p.chunks, unit = blockIdx.x / p.chunks, kvh = unit % p.Hk, b = unit / p.Hk;
   griddep_wait();
   griddep_launch();
+  const int step = p.chunks * SC_WARPS;
+  const bf16* src_hi = reinterpret_cast<const bf16*>(p.k_max) + (size_t)kvh * DH + 8 * t;
+  const bf16* src_lo = reinterpret_cast<const bf16*>(p.k_min) + (size_t)kvh * DH + 8 * t;
+  struct Pages {
+    int at[2];
+  };
+  auto find = [&](int r) {
+    Pages x;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int page = r * 16 + g + 8 * e;
+      x.at[e] = page < p.max_pages ? page_at(p, b, page) : -1;           // (of the table's row: the length is still on its way)
+    }
+    return x;
+  };
+  auto load = [&](uint4 (&x)[2][KC], const bf16* src, const Pages& w) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int j = 0; j < KC; ++j) {
+        x[e][j] = make_uint4(0, 0, 0, 0);
+        if (w.at[e] >= 0) x[e][j] = ld16(src + (size_t)w.at[e] * p.Hk * DH + 32 * j);
+      }
+  };
+  uint4 hi[2][KC], lo[2][KC];
+  int r = chunk * SC_WARPS + warp;
+  Pages now = find(r), then = find(r + step);
   const int N = pages_held(p, b);
   if (N <= p.K) return;                                                  // all of them
   const int tiles = (p.G + 7) / 8;
@@ -83,50 +144,50 @@ __global__ void __launch_bounds__(SC_WARPS * 32) page_score_bf16_kernel(const Se
         h < p.G ? *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(p.q) + (size_t)b * p.q_row + (size_t)(kvh * p.G + h) * p.q_head + c)
                 : make_uint4(0, 0, 0, 0);
   }
+  // (pages behind the last are read as if there were none: stale entries of the table may name any)
+  auto live = [&](Pages& w, int at) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      if (at * 16 + g + 8 * e >= N) w.at[e] = -1;
+  };
+  live(now, r);
+  live(then, r + step);
+  load(hi, src_hi, now);
+  load(lo, src_lo, now);
   __syncthreads();
-  float bound = 0.f;
-  for (int r = chunk * SC_WARPS + warp; r * 16 < N; r += p.chunks * SC_WARPS) {
-    uint4 hi[2][KC], lo[2][KC];
-    int at[2];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int page = r * 16 + g + 8 * e;
-      at[e] = page < N ? page_at(p, b, page) : -1;
-      const size_t from = ((size_t)max(at[e], 0) * p.Hk + kvh) * DH + 8 * t;
-#pragma unroll
-      for (int j = 0; j < KC; ++j) {
-        hi[e][j] = lo[e][j] = make_uint4(0, 0, 0, 0);
-        if (at[e] >= 0) {
-          hi[e][j] = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(p.k_max) + from + 32 * j);
-          lo[e][j] = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(p.k_min) + from + 32 * j);
-        }
-      }
-    }
+  float bound = 0.f, least = INFINITY, most = -INFINITY;
+  bool odd = false;
+  for (; r * 16 < N; r += step) {
     float best[2] = {-INFINITY, -INFINITY};
     bool nan[2] = {false, false};
+    Pages after = find(r + 2 * step);
     for (int n = 0; n < tiles; ++n) {
-      float sh[4] = {0.f, 0.f, 0.f, 0.f}, sl[4] = {0.f, 0.f, 0.f, 0.f}, sb[4] = {0.f, 0.f, 0.f, 0.f};
+      float sh[4] = {0.f, 0.f, 0.f, 0.f}, sl[4] = {0.f, 0.f, 0.f, 0.f}, bh[4] = {0.f, 0.f, 0.f, 0.f}, bl[4] = {0.f, 0.f, 0.f, 0.f};
+      auto multiply = [&](const uint4 (&x)[2][KC], bool up, float (&s)[4], float (&a)[4]) {
 #pragma unroll
-      for (int j = 0; j < KC; ++j) {
-        const uint4 qv = *reinterpret_cast<const uint4*>(q_s + (8 * n + g) * LD + 32 * j + 8 * t);
-        const uint32_t qw[4] = {qv.x, qv.y, qv.z, qv.w};
-        const uint32_t h0[4] = {hi[0][j].x, hi[0][j].y, hi[0][j].z, hi[0][j].w}, h1[4] = {hi[1][j].x, hi[1][j].y, hi[1][j].z, hi[1][j].w};
-        const uint32_t l0[4] = {lo[0][j].x, lo[0][j].y, lo[0][j].z, lo[0][j].w}, l1[4] = {lo[1][j].x, lo[1][j].y, lo[1][j].z, lo[1][j].w};
+        for (int j = 0; j < KC; ++j) {
+          const uint4 qv = *reinterpret_cast<const uint4*>(q_s + (8 * n + g) * LD + 32 * j + 8 * t);
+          const uint32_t qw[4] = {qv.x, qv.y, qv.z, qv.w};
+          const uint32_t x0[4] = {x[0][j].x, x[0][j].y, x[0][j].z, x[0][j].w}, x1[4] = {x[1][j].x, x[1][j].y, x[1][j].z, x[1][j].w};
 #pragma unroll
-        for (int w = 0; w < 4; w += 2) {
-          mma_16816(sh, h0[w], h1[w], h0[w + 1], h1[w + 1], max2(qw[w], 0u), max2(qw[w + 1], 0u));
-          mma_16816(sl, l0[w], l1[w], l0[w + 1], l1[w + 1], min2(qw[w], 0u), min2(qw[w + 1], 0u));
-          mma_16816(sb, max2(abs2(h0[w]), abs2(l0[w])), max2(abs2(h1[w]), abs2(l1[w])), max2(abs2(h0[w + 1]), abs2(l0[w + 1])),
-                    max2(abs2(h1[w + 1]), abs2(l1[w + 1])), abs2(qw[w]), abs2(qw[w + 1]));
+          for (int w = 0; w < 4; w += 2) {
+            const uint32_t q0 = up ? max2(qw[w], 0u) : min2(qw[w], 0u), q1 = up ? max2(qw[w + 1], 0u) : min2(qw[w + 1], 0u);
+            mma_16816(s, x0[w], x1[w], x0[w + 1], x1[w + 1], q0, q1);
+            mma_16816(a, abs2(x0[w]), abs2(x1[w]), abs2(x0[w + 1]), abs2(x1[w + 1]), abs2(q0), abs2(q1));
+          }
         }
-      }
+      };
+      multiply(hi, true, sh, bh);
+      if (n == tiles - 1) load(hi, src_hi, then);
+      multiply(lo, false, sl, bl);
+      if (n == tiles - 1) load(lo, src_lo, then);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (8 * n + 2 * t + (e & 1) >= p.G) continue;
-        const float s = sh[e] + sl[e];
+        const float s = sh[e] + sl[e], a = bh[e] + bl[e];
         nan[e >> 1] |= s != s;
         best[e >> 1] = fmaxf(best[e >> 1], s);
-        if (at[e >> 1] >= 0) bound = sb[e] == sb[e] ? fmaxf(bound, sb[e]) : INFINITY;
+        if (now.at[e >> 1] >= 0) bound = a == a ? fmaxf(bound, a) : INFINITY;
       }
     }
 #pragma unroll
@@ -138,26 +199,31 @@ __global__ void __launch_bounds__(SC_WARPS * 32) page_score_bf16_kernel(const Se
         s = s != s || other != other ? NAN : fmaxf(s, other);
       }
       const int page = r * 16 + g + 8 * e;
-      // (a page that lies nowhere: below every other)
-      if (t == 0 && page < N) p.score[(size_t)unit * p.max_pages + page] = at[e] >= 0 ? s : -INFINITY;
+      if (now.at[e] < 0) s = -INFINITY;                                  // (a page that lies nowhere: below every other)
+      if (page < N) {
+        if (t == 0) p.score[(size_t)unit * p.max_pages + page] = s;
+        if (page >= p.n_first && page < N - p.n_last) {
+          odd |= !(fabsf(s) < INFINITY);
+          least = fminf(least, s);
+          most = fmaxf(most, s);
+        }
+      }
     }
+    now = then;
+    live(after, r + 2 * step);
+    then = after;
   }
-#pragma unroll
-  for (int w = 1; w < 32; w <<= 1) bound = fmaxf(bound, __shfl_xor_sync(0xffffffffu, bound, w));
-  if (lane == 0) s_e[warp] = bound;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < SC_WARPS; ++w) bound = fmaxf(bound, s_e[w]);
-    p.bound[(size_t)unit * p.chunks + chunk] = bound * error_factor<bf16>();
-  }
+  leave_chunk<bf16>(p, unit, chunk, bound, least, most, odd);
 }
 
-// fp32 scores: a page to a warp, DH / 32 elements to a lane.
+// fp32 scores: eight pages to a warp at a time, DH / 32 elements to a lane; the scores of a head and their S are 16 sums over the lanes.
 template <int DH>
-__global__ void __launch_bounds__(SC_WARPS * 32) page_score_f32_kernel(const SelectParams p) {
-  constexpr int E = DH / 32;
+__global__ void __launch_bounds__(SC_WARPS * 32, 4) page_score_f32_kernel(const SelectParams p) {
+  constexpr int E = DH / 32, PAGES = 8;
+  struct alignas(4 * E) Elems {
+    float x[E];
+  };
   extern __shared__ __align__(16) float qf_s[];                          // [heads][DH]
-  __shared__ float s_e[SC_WARPS];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int chunk = blockIdx.x % p.chunks, unit = blockIdx.x / p.chunks, kvh = unit % p.Hk, b = unit / p.Hk;
   griddep_wait();
@@ -167,71 +233,93 @@ __global__ void __launch_bounds__(SC_WARPS * 32) page_score_f32_kernel(const Sel
   for (int i = threadIdx.x; i < p.G * DH; i += SC_WARPS * 32)
     qf_s[i] = reinterpret_cast<const float*>(p.q)[(size_t)b * p.q_row + (size_t)(kvh * p.G + i / DH) * p.q_head + i % DH];
   __syncthreads();
-  float bound = 0.f;
-  for (int page = chunk * SC_WARPS + warp; page < N; page += p.chunks * SC_WARPS) {
-    const int at = page_at(p, b, page);
-    float hi[E], lo[E], best = -INFINITY;
+  const Elems* src_hi = reinterpret_cast<const Elems*>(p.k_max) + (size_t)kvh * 32 + lane;
+  const Elems* src_lo = reinterpret_cast<const Elems*>(p.k_min) + (size_t)kvh * 32 + lane;
+  float bound = 0.f, least = INFINITY, most = -INFINITY;
+  bool odd = false;
+  for (int page0 = (chunk * SC_WARPS + warp) * PAGES; page0 < N; page0 += p.chunks * SC_WARPS * PAGES) {
+    const int mine = page0 + lane < N && lane < PAGES ? page_at(p, b, page0 + lane) : -1;
+    Elems hi[PAGES], lo[PAGES];
+#pragma unroll
+    for (int j = 0; j < PAGES; ++j) {
+      const int at = __shfl_sync(0xffffffffu, mine, j);
+#pragma unroll
+      for (int e = 0; e < E; ++e) hi[j].x[e] = lo[j].x[e] = 0.f;
+      if (at >= 0) {
+        hi[j] = src_hi[(size_t)at * p.Hk * 32];
+        lo[j] = src_lo[(size_t)at * p.Hk * 32];
+      }
+    }
+    float best = -INFINITY, far = 0.f;                                   // lanes 0 .. 15: score of page lane / 2; the others: S of page (lane - 16) / 2
     bool nan = false;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const size_t from = ((size_t)max(at, 0) * p.Hk + kvh) * DH + lane * E + e;
-      hi[e] = at >= 0 ? reinterpret_cast<const float*>(p.k_max)[from] : 0.f;
-      lo[e] = at >= 0 ? reinterpret_cast<const float*>(p.k_min)[from] : 0.f;
-    }
     for (int h = 0; h < p.G; ++h) {
-      float s = 0.f, a = 0.f;
+      const Elems x = *reinterpret_cast<const Elems*>(qf_s + h * DH + lane * E);
+      float s[2 * PAGES];
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float x = qf_s[h * DH + lane * E + e];
-        s = fmaf(x, x >= 0.f ? hi[e] : lo[e], s);
-        a = fmaf(fabsf(x), fmaxf(fabsf(hi[e]), fabsf(lo[e])), a);
-      }
+      for (int j = 0; j < PAGES; ++j) {
+        s[j] = s[PAGES + j] = 0.f;
 #pragma unroll
-      for (int w = 16; w > 0; w >>= 1) {
-        s += __shfl_xor_sync(0xffffffffu, s, w);
-        a += __shfl_xor_sync(0xffffffffu, a, w);
+        for (int e = 0; e < E; ++e) {
+          const float k = x.x[e] >= 0.f ? hi[j].x[e] : lo[j].x[e];
+          s[j] = fmaf(x.x[e], k, s[j]);
+          s[PAGES + j] = fmaf(fabsf(x.x[e]), fabsf(k), s[PAGES + j]);
+        }
       }
-      nan |= s != s;
-      best = fmaxf(best, s);
-      bound = a == a ? fmaxf(bound, a) : INFINITY;
+      halve_sums(s, lane);
+      nan |= s[0] != s[0];
+      best = fmaxf(best, s[0]);
+      far = s[0] == s[0] ? fmaxf(far, s[0]) : INFINITY;
     }
-    if (lane == 0) p.score[(size_t)unit * p.max_pages + page] = at < 0 ? -INFINITY : nan ? NAN : best;
+    const int page = page0 + lane / 2 % PAGES, at = __shfl_sync(0xffffffffu, mine, lane / 2 % PAGES);
+    if (lane >= 16) {
+      if (at >= 0) bound = fmaxf(bound, far);
+    } else if (page < N) {
+      const float s = at < 0 ? -INFINITY : nan ? NAN : best;
+      if (lane % 2 == 0) p.score[(size_t)unit * p.max_pages + page] = s;
+      if (page >= p.n_first && page < N - p.n_last) {
+        odd |= !(fabsf(s) < INFINITY);
+        least = fminf(least, s);
+        most = fmaxf(most, s);
+      }
+    }
   }
-  if (lane == 0) s_e[warp] = bound;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < SC_WARPS; ++w) bound = fmaxf(bound, s_e[w]);
-    p.bound[(size_t)unit * p.chunks + chunk] = bound * error_factor<float>();
-  }
+  leave_chunk<float>(p, unit, chunk, bound, least, most, odd);
 }
 
-// A page's score in fp64, by a warp; a NaN ranks first.
+// A page's score for one head in fp64, by eight lanes (all 32 of the warp call).
 template <typename T> __device__ __forceinline__ double wide(T x);
 template <> __device__ __forceinline__ double wide<float>(float x) { return (double)x; }
 template <> __device__ __forceinline__ double wide<bf16>(bf16 x) { return (double)__bfloat162float(x); }
 template <typename T, int DH>
-__device__ double score_again(const SelectParams& p, int b, int kvh, int page, int lane) {
-  constexpr int E = DH / 32;
+__device__ __forceinline__ double score_again(const SelectParams& p, int b, int kvh, int page, int head, int lane) {
+  constexpr int E = 16 / sizeof(T);                                      // elements of a load
+  struct alignas(16) Elems {
+    T x[E];
+  };
   const int at = page_at(p, b, page);
-  if (at < 0) return -INFINITY;
-  const T* hi = reinterpret_cast<const T*>(p.k_max) + ((size_t)at * p.Hk + kvh) * DH + lane;
-  const T* lo = reinterpret_cast<const T*>(p.k_min) + ((size_t)at * p.Hk + kvh) * DH + lane;
-  double h[E], l[E], best = -INFINITY;
+  const size_t from = ((size_t)max(at, 0) * p.Hk + kvh) * DH + lane % 8 * E;
+  const T* hi = reinterpret_cast<const T*>(p.k_max) + from;
+  const T* lo = reinterpret_cast<const T*>(p.k_min) + from;
+  const T* q = reinterpret_cast<const T*>(p.q) + (size_t)b * p.q_row + (size_t)(kvh * p.G + head) * p.q_head + lane % 8 * E;
+  double s = 0.0;
+  constexpr int J = DH / (8 * E);
+  Elems h[J], l[J], x[J];
 #pragma unroll
-  for (int e = 0; e < E; ++e) { h[e] = wide<T>(hi[32 * e]); l[e] = wide<T>(lo[32 * e]); }
-  for (int g = 0; g < p.G; ++g) {
-    const T* q = reinterpret_cast<const T*>(p.q) + (size_t)b * p.q_row + (size_t)(kvh * p.G + g) * p.q_head + lane;
-    double s = 0.0;
+  for (int j = 0; j < J; ++j) {
+    h[j] = *reinterpret_cast<const Elems*>(hi + j * 8 * E);
+    l[j] = *reinterpret_cast<const Elems*>(lo + j * 8 * E);
+    x[j] = *reinterpret_cast<const Elems*>(q + j * 8 * E);
+  }
+#pragma unroll
+  for (int j = 0; j < J; ++j)
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const double x = wide<T>(q[32 * e]), a = x * l[e], c = x * h[e];
+      const double y = wide<T>(x[j].x[e]), a = y * wide<T>(l[j].x[e]), c = y * wide<T>(h[j].x[e]);
       s += a != a || c != c ? a + c : fmax(a, c);
     }
 #pragma unroll
-    for (int w = 16; w > 0; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
-    best = s != s || best != best ? (double)NAN : fmax(best, s);
-  }
-  return best != best ? (double)INFINITY : best;
+  for (int w = 4; w > 0; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
+  return at < 0 ? -INFINITY : s;
 }
 
 // Order-preserving images of floats and doubles.
@@ -242,18 +330,22 @@ __device__ __forceinline__ int ordered(float x) {
 __device__ __forceinline__ float from_ordered(int i) { return __int_as_float(i >= 0 ? i : i ^ 0x7fffffff); }
 __device__ __forceinline__ unsigned long long ordered(double x) {
   if (x == 0.0) x = 0.0;                                                 // (one zero)
+  if (x != x) x = INFINITY;                                              // (what is not a number ranks first)
   const unsigned long long i = (unsigned long long)__double_as_longlong(x);
   return i >> 63 ? ~i : i | 0x8000000000000000ull;
 }
 
 __device__ __forceinline__ int block_sum(int v, int* red) {
+  constexpr int WARPS = SEL_THREADS / 32;
+  const int lane = threadIdx.x & 31;
   v = __reduce_add_sync(0xffffffffu, v);
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+  if (lane == 0) red[threadIdx.x >> 5] = v;
   __syncthreads();
-  return __reduce_add_sync(0xffffffffu, red[threadIdx.x & 31]);
+  return __reduce_add_sync(0xffffffffu, lane < WARPS ? red[lane] : 0);
 }
 __device__ __forceinline__ int block_scan(int v, int* red, int& total) {     // exclusive
+  constexpr int WARPS = SEL_THREADS / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int s = v;
 #pragma unroll
@@ -264,92 +356,112 @@ __device__ __forceinline__ int block_scan(int v, int* red, int& total) {     // 
   __syncthreads();
   if (lane == 31) red[warp] = s;
   __syncthreads();
-  int w = red[lane];
+  int w = lane < WARPS ? red[lane] : 0;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
+  for (int o = 1; o < WARPS; o <<= 1) {
     const int u = __shfl_up_sync(0xffffffffu, w, o);
     if (lane >= o) w += u;
   }
-  total = __shfl_sync(0xffffffffu, w, 31);
+  total = __shfl_sync(0xffffffffu, w, WARPS - 1);
   const int before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
   return s - v + (warp ? before : 0);
 }
 
 // One CTA per (sequence, KV head).  The border is closed in on by histograms between the smallest and the largest score (a bin is a range of values; a score's
 // bin is a monotonic function of it), each level in the range of the bin that holds the border, until few pages are left in it; those, and
-// what lies within 2 E of them, are ranked in fp64.
+// what lies within 2 E of them, are ranked in fp64.  Scores of up to SEL_KEEP pages stay in shared memory, those of more are read again at every pass.
+// With a CTA to an SM, each of its instructions executed a few times, much of the time is that of fetching them: the loops stay rolled.  (Unrolled, with
+// the scores in registers, the histogram of 2000 pages took as long as that of 8192, 3 us.)
 template <typename T, int DH>
-__global__ void __launch_bounds__(SEL_THREADS, 1) page_select_kernel(const SelectParams p) {
-  extern __shared__ __align__(16) float score_s[];
+__global__ void __launch_bounds__(SEL_THREADS, 2) page_select_kernel(const SelectParams p) {
   __shared__ int red[32], hist[SEL_BINS];
   __shared__ unsigned taken[kMaxSelectPages / 32];
   __shared__ int list[SEL_LIST];
-  __shared__ double again[SEL_LIST];
-  __shared__ int s_lo, s_hi, s_n, s_bin, s_above;
+  __shared__ unsigned long long again[SEL_LIST];
+  __shared__ int s_lo, s_hi, s_n, s_bin, s_above, s_bound, s_odd;
+  extern __shared__ float kept[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int unit = blockIdx.x, kvh = unit % p.Hk, b = unit / p.Hk;
+  if (tid == 0) {
+    s_lo = ordered(INFINITY);
+    s_hi = ordered(-INFINITY);
+    s_n = s_bound = s_odd = 0;
+  }
+  hist[tid] = 0;
   griddep_wait();
   griddep_launch();
+  // what does not need the length is on its way before it: the scores (of the whole table's row, whatever lies behind the last) and what is known of them
+  const float* score = p.score + (size_t)unit * p.max_pages;
+  for (int i = tid; i < min(p.max_pages, SEL_KEEP); i += SEL_THREADS)
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(kept + i)), "l"(score + i) : "memory");
+  const bool counts = tid / 32 * 32 < p.chunks;
+  float4 known = make_float4(0.f, INFINITY, -INFINITY, 0.f);
+  if (tid < p.chunks) known = *reinterpret_cast<const float4*>(&p.chunk[(size_t)unit * p.chunks + tid]);
   const int N = pages_held(p, b), n = min(N, p.K);
   int32_t* sel = p.sel + (size_t)unit * p.K;
   if (kvh == 0 && tid == 0) p.n_sel[b] = n;
   for (int i = n + tid; i < p.K; i += SEL_THREADS) sel[i] = -1;
   if (N <= p.K) {
     for (int i = tid; i < N; i += SEL_THREADS) sel[i] = i;
+    asm volatile("cp.async.wait_all;" ::: "memory");
     return;
   }
   const int first = p.n_first, last = N - p.n_last;                      // pages first .. last - 1 are up for selection
   const int want = p.K - first - p.n_last;                               // (K >= n_first + n_last, and N > K)
+  const bool keep = N <= SEL_KEEP;
+  // f(page, score) for this thread's pages
+  auto each = [&](auto f) {
+    if (keep) {
+#pragma unroll 1
+      for (int i = first + tid; i < last; i += 4 * SEL_THREADS) {
+        float s[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] = i + j * SEL_THREADS < last ? kept[i + j * SEL_THREADS] : 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (i + j * SEL_THREADS < last) f(i + j * SEL_THREADS, s[j]);
+      }
+    } else {
+#pragma unroll 1
+      for (int i = first + tid; i < last; i += SEL_THREADS) f(i, score[i]);
+    }
+  };
   const int words = (N + 31) / 32;
-  for (int i = tid; i < words; i += SEL_THREADS) {
-    // the forced ones
-    unsigned m = 0;
-    for (int j = 0; j < 32; ++j) {
-      const int page = i * 32 + j;
-      if (page < N && (page < first || page >= last)) m |= 1u << j;
-    }
-    taken[i] = m;
-  }
-  if (tid == 0) { s_lo = ordered(INFINITY); s_hi = ordered(-INFINITY); s_n = 0; }
-  float bound = 0.f;
-  for (int i = tid; i < p.chunks; i += SEL_THREADS) bound = fmaxf(bound, p.bound[(size_t)unit * p.chunks + i]);
+  auto below = [](int pages, int word) { return pages >= word * 32 + 32 ? 0xffffffffu : pages <= word * 32 ? 0u : (1u << (pages - word * 32)) - 1; };
+  for (int i = tid; i < words; i += SEL_THREADS) taken[i] = below(first, i) | (below(N, i) & ~below(last, i));    // the ones that are always taken
   __syncthreads();
-  const float* score = p.score + (size_t)unit * p.max_pages;
-  {
-    float lo = INFINITY, hi = -INFINITY;
-    int odd = 0;
-    for (int i = first + tid; i < last; i += SEL_THREADS) {
-      const float s = score[i];
-      if (N <= SEL_SMEM_PAGES) score_s[i] = s;
-      if (!(fabsf(s) < INFINITY)) ++odd;
-      lo = fminf(lo, s);
-      hi = fmaxf(hi, s);
+  if (counts) {
+    const int lw = __reduce_min_sync(0xffffffffu, ordered(known.y)), hw = __reduce_max_sync(0xffffffffu, ordered(known.z));
+    const int e = __reduce_max_sync(0xffffffffu, __float_as_int(known.x));     // (not negative, not a NaN)
+    const bool odd = __any_sync(0xffffffffu, __float_as_int(known.w) != 0);
+    if (lane == 0) {
+      atomicMin(&s_lo, lw);
+      atomicMax(&s_hi, hw);
+      atomicMax(&s_bound, e);
+      if (odd) s_odd = 1;
     }
-    const int l = __reduce_min_sync(0xffffffffu, ordered(lo)), h = __reduce_max_sync(0xffffffffu, ordered(hi));
-    const int e = __reduce_max_sync(0xffffffffu, __float_as_int(bound));   // (not negative, not a NaN)
-    if (lane == 0) { atomicMin(&s_lo, l); atomicMax(&s_hi, h); red[warp] = e; }
-    odd = __reduce_add_sync(0xffffffffu, odd);
-    if (lane == 0 && odd) atomicAdd(&s_n, odd);
   }
+  asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
-  const float E = __int_as_float(__reduce_max_sync(0xffffffffu, red[lane]));
-  if (N <= SEL_SMEM_PAGES) score = score_s;
+  const float E = __int_as_float(s_bound);
   float lo = from_ordered(s_lo), hi = from_ordered(s_hi);
-  const bool all_again = s_n > 0 || !(E < INFINITY);                     // scores that are not finite decide nothing
+  const bool all_again = s_odd || !(E < INFINITY);                       // scores that are not finite decide nothing
   int above = 0;                                                         // pages above hi
   float t_lo = -INFINITY, t_hi = INFINITY;
   if (!all_again && want > 0) {
+#pragma unroll 1
     for (int level = 0; level < 8; ++level) {
-      __syncthreads();
-      for (int i = tid; i < SEL_BINS; i += SEL_THREADS) hist[i] = 0;
-      __syncthreads();
       const float inv = (float)SEL_BINS / (hi - lo);
-      auto bin_of = [&](float s) { return min(SEL_BINS - 1, max(0, (int)((s - lo) * inv))); };
       if (!(hi > lo) || !(inv < INFINITY)) break;
-      for (int i = first + tid; i < last; i += SEL_THREADS) {
-        const float s = score[i];
-        if (s >= lo && s <= hi) atomicAdd(&hist[bin_of(s)], 1);
+      auto bin_of = [&](float s) { return min(SEL_BINS - 1, max(0, (int)((s - lo) * inv))); };
+      if (level) {
+        __syncthreads();
+        hist[tid] = 0;
+        __syncthreads();
       }
+      each([&](int, float s) {
+        if (s >= lo && s <= hi) atomicAdd(&hist[bin_of(s)], 1);
+      });
       __syncthreads();
       // the bin with the want-th best: thread i looks at the i-th bin from above
       static_assert(SEL_BINS == SEL_THREADS, "a bin per thread");
@@ -359,85 +471,92 @@ __global__ void __launch_bounds__(SEL_THREADS, 1) page_select_kernel(const Selec
       if (before < want && before + mine >= want) { s_bin = SEL_BINS - 1 - tid; s_above = before; s_lo = ordered(INFINITY); s_hi = ordered(-INFINITY); }
       __syncthreads();
       const int bin = s_bin, count = hist[bin];
-      float l = INFINITY, h = -INFINITY;
-      for (int i = first + tid; i < last; i += SEL_THREADS) {
-        const float s = score[i];
-        if (s >= lo && s <= hi && bin_of(s) == bin) { l = fminf(l, s); h = fmaxf(h, s); }
-      }
-      const int lw = __reduce_min_sync(0xffffffffu, ordered(l)), hw = __reduce_max_sync(0xffffffffu, ordered(h));
-      if (lane == 0) { atomicMin(&s_lo, lw); atomicMax(&s_hi, hw); }
-      __syncthreads();
       above = s_above;
+      if (count <= 32) {
+        // the bin's edges, and more than what rounding can have moved a score across them
+        const float slack = 4e-7f * (fabsf(lo) + fabsf(hi)), from = lo;
+        lo = from + (float)bin / inv - slack;
+        hi = from + (float)(bin + 1) / inv + slack;
+        break;
+      }
+      float l = INFINITY, h = -INFINITY;
+      each([&](int, float s) {
+        if (s >= lo && s <= hi && bin_of(s) == bin) { l = fminf(l, s); h = fmaxf(h, s); }
+      });
+      if (__any_sync(0xffffffffu, l <= h)) {
+        const int lw = __reduce_min_sync(0xffffffffu, ordered(l)), hw = __reduce_max_sync(0xffffffffu, ordered(h));
+        if (lane == 0) { atomicMin(&s_lo, lw); atomicMax(&s_hi, hw); }
+      }
+      __syncthreads();
       lo = from_ordered(s_lo);
       hi = from_ordered(s_hi);
-      if (count <= 32 || hi - lo <= E) break;
+      if (hi - lo <= E) break;
     }
     t_lo = lo - 2.1f * E;
     t_hi = hi + 2.1f * E;
   }
   // sure ones and those near the border
-  __syncthreads();
-  if (tid == 0) s_n = 0;
-  __syncthreads();
   int sure = 0;
   if (want > 0)
-    for (int i = first + tid; i < last; i += SEL_THREADS) {
-      const float s = score[i];
+    each([&](int i, float s) {
       if (!all_again && s > t_hi) {
         atomicOr(&taken[i >> 5], 1u << (i & 31));
         ++sure;
       } else if (all_again || s >= t_lo) {
         const int at = atomicAdd(&s_n, 1);
-        if (at < SEL_LIST) list[at] = i;
+        if (at < SEL_LIST) { list[at] = i; again[at] = 0; }
       }
-    }
+    });
   sure = block_sum(sure, red);
   const int near = s_n, rest = want - sure;
-  if (near == rest || near <= SEL_LIST) {
+  if (near <= SEL_LIST) {
     if (near > rest) {
-      for (int i = warp; i < near; i += SEL_THREADS / 32) {
-        const double s = score_again<T, DH>(p, b, kvh, list[i], lane);
-        if (lane == 0) again[i] = s;
+#pragma unroll 1
+      for (int i0 = warp * 4; i0 < near * p.G; i0 += SEL_THREADS / 8) {
+        const int i = i0 + lane / 8, w = min(i, near * p.G - 1);
+        const double s = score_again<T, DH>(p, b, kvh, list[w / p.G], w % p.G, lane);
+        if (lane % 8 == 0 && i == w) atomicMax(&again[w / p.G], ordered(s));
       }
       __syncthreads();
-      for (int i = tid; i < near; i += SEL_THREADS) {
-        int rank = 0;
+    }
+    for (int i = tid; i < near; i += SEL_THREADS) {
+      int rank = 0;
+      if (near > rest)
+#pragma unroll 1
         for (int j = 0; j < near; ++j) rank += again[j] > again[i] || (again[j] == again[i] && list[j] < list[i]);
-        if (rank < rest) atomicOr(&taken[list[i] >> 5], 1u << (list[i] & 31));
-      }
-    } else if (near <= SEL_LIST) {
-      for (int i = tid; i < near; i += SEL_THREADS) atomicOr(&taken[list[i] >> 5], 1u << (list[i] & 31));
-    } else {
-      for (int i = first + tid; i < last; i += SEL_THREADS)
-        if (all_again || score[i] >= t_lo) atomicOr(&taken[i >> 5], 1u << (i & 31));
+      if (rank < rest) atomicOr(&taken[list[i] >> 5], 1u << (list[i] & 31));
     }
   } else {
     // many near the border (a cache of equal keys, scores that are not finite): all of them in fp64, the border by bisection of the ordered values
-    double* far = p.again + (size_t)unit * p.max_pages;
+    unsigned long long* far = p.again + (size_t)unit * p.max_pages;
     auto is_near = [&](int i) { return all_again || (score[i] >= t_lo && score[i] <= t_hi); };
-    for (int i = first + warp; i < last; i += SEL_THREADS / 32)
-      if (is_near(i)) {
-        const double s = score_again<T, DH>(p, b, kvh, i, lane);
-        if (lane == 0) far[i] = s;
-      }
+#pragma unroll 1
+    for (int i0 = first + warp * 4; i0 < last; i0 += SEL_THREADS / 8) {
+      const int i = min(i0 + lane / 8, last - 1);
+      unsigned long long best = 0;
+#pragma unroll 1
+      for (int h = 0; h < p.G; ++h) best = max(best, ordered(score_again<T, DH>(p, b, kvh, i, h, lane)));
+      if (lane % 8 == 0) far[i] = best;
+    }
     __syncthreads();
     unsigned long long v = 0;                                            // the largest that `rest` or more are not below
     for (int bit = 63; bit >= 0; --bit) {
       const unsigned long long c = v | 1ull << bit;
       int cnt = 0;
-      for (int i = first + tid; i < last; i += SEL_THREADS) cnt += is_near(i) && ordered(far[i]) >= c;
+#pragma unroll 4
+      for (int i = first + tid; i < last; i += SEL_THREADS) cnt += is_near(i) && far[i] >= c;
       if (block_sum(cnt, red) >= rest) v = c;
     }
     int over = 0;
     for (int i = first + tid; i < last; i += SEL_THREADS)
-      if (is_near(i) && ordered(far[i]) > v) {
+      if (is_near(i) && far[i] > v) {
         atomicOr(&taken[i >> 5], 1u << (i & 31));
         ++over;
       }
     int ties = rest - block_sum(over, red);
     for (int i0 = first; i0 < last && ties > 0; i0 += SEL_THREADS) {
       const int i = i0 + tid;
-      const int tie = i < last && is_near(i) && ordered(far[i]) == v;
+      const int tie = i < last && is_near(i) && far[i] == v;
       int total;
       const int before = block_scan(tie, red, total);
       if (tie && before < ties) atomicOr(&taken[i >> 5], 1u << (i & 31));
@@ -459,13 +578,13 @@ int plan_select(int dtype, int B, int H, int Hk, int head_dim, int max_pages, si
   if (B < 0 || H < 1 || Hk < 1 || H % Hk || (head_dim != 64 && head_dim != 128) || max_pages < 1 || max_pages > kMaxSelectPages) return CERB_E_SHAPE;
   if (H / Hk > 64 || (long long)B * Hk > 0x7fffffll) return CERB_E_SHAPE;
   const long long units = (long long)B * Hk;
-  // CTAs for every SM a few times over, of no less than a round of their warps
-  const int held = (int)(((long long)max_len + CERB_PAGE - 1) / CERB_PAGE), per = dtype == CERB_BF16 ? 16 * SC_WARPS : SC_WARPS;
-  const long long most = (std::min(held, max_pages) + per - 1) / per, want = units ? (148 * 8 + units - 1) / units : 1;
-  *chunks = (int)std::max(1ll, std::min(most, want));
+  // as many CTAs as run at once, of no less than a round of their warps
+  const int held = (int)(((long long)max_len + CERB_PAGE - 1) / CERB_PAGE), per = (dtype == CERB_BF16 ? 16 : 8) * SC_WARPS;
+  const long long most = (std::min(held, max_pages) + per - 1) / per, want = units ? 148 * (dtype == CERB_BF16 ? 3 : 4) / units : 1;
+  *chunks = (int)std::max(1ll, std::min({most, want, (long long)SEL_THREADS}));
   *score_bytes = ((size_t)units * max_pages * sizeof(float) + 255) & ~(size_t)255;
-  *bound_bytes = ((size_t)units * *chunks * sizeof(float) + 255) & ~(size_t)255;
-  *again_bytes = (size_t)units * max_pages * sizeof(double);
+  *bound_bytes = ((size_t)units * *chunks * sizeof(ChunkScores) + 255) & ~(size_t)255;
+  *again_bytes = (size_t)units * max_pages * sizeof(unsigned long long);
   return CERB_OK;
 }
 
@@ -509,8 +628,8 @@ int cerb_page_select(const cerb_page_select_args* a, void* stream) {
   p.sel = a->sel;
   p.n_sel = a->n_sel;
   p.score = (float*)a->scratch;
-  p.bound = (float*)((char*)a->scratch + s);
-  p.again = (double*)((char*)a->scratch + s + e);
+  p.chunk = (ChunkScores*)((char*)a->scratch + s);
+  p.again = (unsigned long long*)((char*)a->scratch + s + e);
   p.q_row = a->q_row_stride;
   p.q_head = a->q_head_stride;
   p.B = a->B;
@@ -531,9 +650,8 @@ int cerb_page_select(const cerb_page_select_args* a, void* stream) {
   if (launch_pdl(score, dim3(units * (unsigned)chunks), dim3(SC_WARPS * 32), q_smem, st, p) != cudaSuccess) return CERB_E_CUDA;
   auto kern = bf ? (big ? page_select_kernel<bf16, 128> : page_select_kernel<bf16, 64>) : (big ? page_select_kernel<float, 128> : page_select_kernel<float, 64>);
   static std::atomic<uint64_t> done[4];
-  CERB_TRY(allow_smem(kern, done[2 * bf + big], SEL_SMEM_PAGES * (int)sizeof(float)));
-  const int held = (int)std::min((long long)a->max_pages, (long long)SEL_SMEM_PAGES);
-  return launch_pdl(kern, dim3(units), dim3(SEL_THREADS), (size_t)held * sizeof(float), st, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
+  CERB_TRY(allow_smem(kern, done[2 * bf + big], SEL_KEEP * (int)sizeof(float)));
+  return launch_pdl(kern, dim3(units), dim3(SEL_THREADS), std::min(a->max_pages, SEL_KEEP) * sizeof(float), st, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
 }
 
 }  // extern "C"

@@ -11,6 +11,7 @@
 
 #include <algorithm>
 
+#include "paged_common.cuh"
 #include "tc_common.cuh"
 
 namespace cerb {
@@ -18,7 +19,7 @@ namespace cerb {
 namespace {
 
 constexpr int PA_WARPS = 4;
-constexpr int PA_CLUSTER = 8;         // CTAs of a cluster at most
+constexpr int PA_CLUSTER = 16;        // CTAs of a cluster at most (more than eight: where the device lets them)
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct PagedParams {
@@ -50,17 +51,21 @@ __device__ __forceinline__ Span span_of(const PagedParams& p, int b) {
   return s;
 }
 
-// The page of an item: its number among the sequence's, and where it lies (-1: nothing to read there).
+// The page of an item: its number among the sequence's, and where it lies (-1: nowhere in the pool).  Needs the sequence's length only for `first`: what lies
+// behind it, or behind the list, is for the caller to leave out.
 struct PageRef {
   int page, at;
 };
-__device__ __forceinline__ PageRef page_ref(const PagedParams& p, const Span& s, int b, int kvh, int item) {
+__device__ __forceinline__ PageRef page_ref(const PagedParams& p, int first, int b, int kvh, int item) {
   PageRef r{-1, -1};
-  if (item >= s.items) return r;
-  r.page = p.sel ? p.sel[((size_t)b * p.Hk + kvh) * p.max_sel + item] : s.first + item;
-  if (r.page < 0 || r.page >= (s.hi + CERB_PAGE - 1) / CERB_PAGE) return r;
+  if (p.sel) {
+    if (item < p.max_sel) r.page = p.sel[((size_t)b * p.Hk + kvh) * p.max_sel + item];
+  } else {
+    r.page = first + item;
+  }
+  if (r.page < 0 || r.page >= p.max_pages) return r;
   const int at = p.page_table[(size_t)b * p.max_pages + r.page];
-  if (at >= 0 && at < p.n_pool_pages) r.at = at;
+  if (at < p.n_pool_pages) r.at = at;
   return r;
 }
 
@@ -154,17 +159,36 @@ __device__ __forceinline__ void store_out(const PagedParams& p, size_t row, int 
   if (d == 0 && p.lse) p.lse[row] = (m + log2f(l)) * kLn2;
 }
 
-// A piece of a unit: some of its items, for these of the query heads.
+// A piece of a unit: the items from item0 up to item1, of which a warp takes every stride-th, for these of the query heads.
 struct Piece {
   Span sp;
-  int b, kvh, head0, heads, item0, item1;
+  int b, kvh, head0, heads, item0, item1, stride;
+  PageRef ahead;                  // of this lane's item among the warp's first 32
+};
+__device__ __forceinline__ int warp_item(const Piece& c, int i) { return c.item0 + (int)(threadIdx.x >> 5) + i * c.stride; }
+// The pages that a warp goes through, looked up 32 at a time.
+struct Walk {
+  int i = 0, mine, pages_l = -1, at_l = -1;
+  __device__ __forceinline__ explicit Walk(const Piece& c) : mine(max(0, (c.item1 - warp_item(c, 0) + c.stride - 1) / c.stride)) {}
+  // the next one that there is something to read of, or {-1, -1}
+  __device__ __forceinline__ PageRef next(const PagedParams& p, const Piece& c) {
+    const int lane = threadIdx.x & 31;
+    PageRef r{-1, -1};
+    while (i < mine) {
+      if (i % 32 == 0) {
+        const PageRef l = i == 0 ? c.ahead : page_ref(p, c.sp.first, c.b, c.kvh, warp_item(c, i + lane));
+        pages_l = l.page;
+        at_l = i + lane < mine && (unsigned)l.page < (unsigned)((c.sp.hi + CERB_PAGE - 1) / CERB_PAGE) ? l.at : -1;
+      }
+      r.page = __shfl_sync(0xffffffffu, pages_l, i % 32);
+      r.at = __shfl_sync(0xffffffffu, at_l, i % 32);
+      ++i;
+      if (r.at >= 0) break;
+    }
+    return r;
+  }
 };
 
-__device__ __forceinline__ uint4 ld16(const void* src) {
-  uint4 r;
-  asm volatile("ld.global.L1::no_allocate.L2::256B.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(src) : "memory");
-  return r;
-}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -191,27 +215,10 @@ __device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c
   const bf16* kp = reinterpret_cast<const bf16*>(p.k_pool) + (size_t)c.kvh * CERB_PAGE * DH + g * DH + t * 8;
   const bf16* vp = reinterpret_cast<const bf16*>(p.v_pool) + (size_t)c.kvh * CERB_PAGE * DH + 2 * t * DH + g * 8;
   const size_t page_elems = (size_t)p.Hk * CERB_PAGE * DH;
-  // this warp's items: every PA_WARPS-th; the pages of 32 of them are looked up at once
-  int i = 0, pages_l = -1, at_l = -1;
-  const int mine = max(0, (c.item1 - c.item0 - warp + PA_WARPS - 1) / PA_WARPS);
-  auto next = [&]() {
-    PageRef r{-1, -1};
-    while (i < mine) {
-      if (i % 32 == 0) {
-        const PageRef l = i + lane < mine ? page_ref(p, c.sp, c.b, c.kvh, c.item0 + (i + lane) * PA_WARPS + warp) : PageRef{-1, -1};
-        pages_l = l.page;
-        at_l = l.at;
-      }
-      r.page = __shfl_sync(0xffffffffu, pages_l, i % 32);
-      r.at = __shfl_sync(0xffffffffu, at_l, i % 32);
-      ++i;
-      if (r.at >= 0) break;                                              // (there is something to read of it)
-    }
-    return r;
-  };
+  Walk walk(c);
   PageRef now[KP], then[KP];
 #pragma unroll
-  for (int a = 0; a < KP; ++a) now[a] = next();
+  for (int a = 0; a < KP; ++a) now[a] = walk.next(p, c);
   uint4 k[KP][2][KC], v[KP][4][VH];
   auto load_k = [&](const PageRef (&r)[KP]) {
 #pragma unroll
@@ -251,7 +258,7 @@ __device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c
   }
   while (now[0].at >= 0) {
 #pragma unroll
-    for (int a = 0; a < KP; ++a) then[a] = next();
+    for (int a = 0; a < KP; ++a) then[a] = walk.next(p, c);
     float s[KP][NT][4];
 #pragma unroll
     for (int a = 0; a < KP; ++a)
@@ -362,28 +369,8 @@ __device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c
 }
 
 // fp32: plain FMA.  A lane owns DH / 32 elements of every key and value, a warp takes KEYS keys at a time for up to GH heads and has the next ones on their way.
-// The lanes' KEYS x GH partial sums meet by halving (every exchange carries half of what is left: as many shuffles as sums), after which each lane has the
-// scores of few keys to take the exponential of; the weights come back by shuffles.
-template <int N>
-__device__ __forceinline__ void halve_sums(float (&x)[N], int lane) {
-  int n = N;
-#pragma unroll
-  for (int w = 16; w > 0; w >>= 1) {
-    if (n > 1) {
-      n >>= 1;
-      const bool up = lane & w;
-#pragma unroll
-      for (int i = 0; i < N / 2; ++i)
-        if (i < n) {
-          const float send = up ? x[i] : x[i + n], keep = up ? x[i + n] : x[i];
-          x[i] = keep + __shfl_xor_sync(0xffffffffu, send, w);
-        }
-    } else {
-      x[0] += __shfl_xor_sync(0xffffffffu, x[0], w);
-    }
-  }
-}
-
+// The lanes' KEYS x GH partial sums meet by halving, after which each lane has the scores of few keys to take the exponential of; the weights come back by
+// shuffles.
 template <int DH, int GH>
 __device__ __forceinline__ void attend_f32(const PagedParams& p, const Piece& c, Sums<DH, GH>& sums) {
   constexpr int E = DH / 32, KEYS = DH == 64 && GH <= 2 ? 16 : 8, STEPS = CERB_PAGE / KEYS;
@@ -405,9 +392,9 @@ __device__ __forceinline__ void attend_f32(const PagedParams& p, const Piece& c,
         asm volatile("ld.global.L1::no_allocate.L2::256B.v2.f32 {%0, %1}, [%2];" : "=f"(r[j].x[0]), "=f"(r[j].x[1]) : "l"(src + j * DH) : "memory");
     }
   };
-  // this warp's steps: every PA_WARPS-th item, the parts of a page that have a live row
-  int i = 0, step = STEPS, pages_l = -1, at_l = -1;
-  const int mine = max(0, (c.item1 - c.item0 - warp + PA_WARPS - 1) / PA_WARPS);
+  // this warp's steps: the parts of its pages that have a live row
+  Walk walk(c);
+  int step = STEPS;
   PageRef page{-1, -1};
   struct Step {
     int row0;
@@ -416,16 +403,8 @@ __device__ __forceinline__ void attend_f32(const PagedParams& p, const Piece& c,
   auto next = [&]() {
     for (;;) {
       if (step == STEPS) {
-        if (i >= mine) return Step{0, -1};
-        if (i % 32 == 0) {
-          const PageRef l = i + lane < mine ? page_ref(p, c.sp, c.b, c.kvh, c.item0 + (i + lane) * PA_WARPS + warp) : PageRef{-1, -1};
-          pages_l = l.page;
-          at_l = l.at;
-        }
-        page.page = __shfl_sync(0xffffffffu, pages_l, i % 32);
-        page.at = __shfl_sync(0xffffffffu, at_l, i % 32);
-        ++i;
-        if (page.at < 0) continue;
+        page = walk.next(p, c);
+        if (page.at < 0) return Step{0, -1};
         step = 0;
       }
       const int row0 = page.page * CERB_PAGE + step * KEYS;
@@ -540,6 +519,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_
   bool left = !p.by_unit;                                                // this CTA's join is still to be said
   Piece c;
   c.b = sh.b;
+  c.stride = PA_WARPS;
   long long off = sh.off;
   for (long long at = sh.begin; at < sh.end;) {
     c.sp = span_of(p, c.b);
@@ -554,6 +534,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_
     const int n = (int)min((long long)(items - c.item0), sh.end - at);
     c.item1 = c.item0 + n;
     c.kvh = u / p.units_h;
+    c.ahead = page_ref(p, c.sp.first, c.b, c.kvh, warp_item(c, threadIdx.x & 31));
     const int part = u - c.kvh * p.units_h, unit = (int)(c.b * uh) + u;
     c.head0 = c.kvh * p.G + part * HEADS;
     c.heads = min(HEADS, p.G - part * HEADS);
@@ -601,10 +582,14 @@ __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_
   c.heads = min(HEADS, p.G - part * HEADS);
   griddep_wait();
   griddep_launch();
+  // (the items are dealt out one by one, so that the first ones can be looked up before the length is known)
+  c.item0 = rank * PA_WARPS;
+  c.stride = n * PA_WARPS;
+  if (p.window == 0 || p.sel) c.ahead = page_ref(p, 0, c.b, c.kvh, warp_item(c, threadIdx.x & 31));
   c.sp = span_of(p, c.b);
-  const int per = (c.sp.items + n - 1) / n, own = HEADS * DH / n;
-  c.item0 = min(c.sp.items, rank * per);
-  c.item1 = min(c.sp.items, c.item0 + per);
+  if (p.window > 0 && !p.sel) c.ahead = page_ref(p, c.sp.first, c.b, c.kvh, warp_item(c, threadIdx.x & 31));
+  c.item1 = c.sp.items;
+  const int own = HEADS * DH / n;
   attend<T, DH, HEADS>(p, c, sums);
   __syncthreads();
   cluster_start_wait();                                                  // every CTA of the cluster runs
@@ -742,6 +727,10 @@ size_t scratch_bytes(const PagedPlan& g, int head_dim) {
 template <typename T, int DH, int HEADS>
 cudaError_t launch(const PagedPlan& g, const PagedParams& p, cudaStream_t st) {
   const dim3 block(PA_WARPS * 32);
+  if (g.together > 8) {
+    static std::atomic<uint64_t> done{0};
+    if (allow_wide_clusters(paged_attn_cluster_kernel<T, DH, HEADS>, done) != CERB_OK) return cudaErrorInvalidValue;
+  }
   if (g.together) return launch_pdl_cluster(paged_attn_cluster_kernel<T, DH, HEADS>, dim3((unsigned)g.ctas), block, 0, st, (unsigned)g.together, p);
   const cudaError_t rc = launch_pdl(paged_attn_kernel<T, DH, HEADS>, dim3((unsigned)g.ctas), block, 0, st, p);
   if (rc != cudaSuccess || g.ctas == 1) return rc;
