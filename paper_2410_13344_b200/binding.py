@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libcerb.so (include/cerb.h): argument marshalling only.
+"""Thin ctypes binding of libcerb.so (include/cerb.h): argument marshalling only (of the paged-cache calls natively, in _paged.so).
 
 Every step of the decoding path runs in the library's CUDA kernels; torch is used
 here for device memory and streams.  Importing this module fails loudly if the
@@ -7,7 +7,6 @@ shared library has not been built -- there is no fallback path.
 from __future__ import annotations
 
 import ctypes as C
-import functools
 import os
 from typing import Dict, List, NamedTuple, Optional, Sequence
 
@@ -85,44 +84,6 @@ class AttnArgs(C.Structure):
     ]
 
 
-class Pages(C.Structure):
-    _fields_ = [
-        ("B", C.c_int32), ("max_pages", C.c_int32), ("free_cap", C.c_int32),
-        ("len", C.c_void_p), ("page_table", C.c_void_p), ("free_pages", C.c_void_p), ("n_free", C.c_void_p),
-    ]
-
-
-class KvAppendArgs(C.Structure):
-    _fields_ = [
-        ("dtype", C.c_int32), ("T", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
-        ("k", C.c_void_p), ("v", C.c_void_p),
-        ("k_row_stride", C.c_int64), ("k_head_stride", C.c_int64), ("v_row_stride", C.c_int64), ("v_head_stride", C.c_int64),
-        ("slot", C.c_void_p), ("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("k_min", C.c_void_p), ("k_max", C.c_void_p),
-        ("n_pool_pages", C.c_int32),
-    ]
-
-
-class PagedAttnArgs(C.Structure):
-    _fields_ = [
-        ("dtype", C.c_int32), ("B", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
-        ("max_pages", C.c_int32), ("n_pool_pages", C.c_int32),
-        ("q", C.c_void_p), ("q_row_stride", C.c_int64), ("q_head_stride", C.c_int64), ("k_pool", C.c_void_p), ("v_pool", C.c_void_p),
-        ("page_table", C.c_void_p), ("len", C.c_void_p), ("sel", C.c_void_p), ("n_sel", C.c_void_p), ("max_sel", C.c_int32),
-        ("out", C.c_void_p), ("lse", C.c_void_p), ("scale", C.c_float), ("max_len", C.c_int32), ("window", C.c_int32),
-        ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t),
-    ]
-
-
-class PageSelectArgs(C.Structure):
-    _fields_ = [
-        ("dtype", C.c_int32), ("B", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
-        ("max_pages", C.c_int32), ("n_pool_pages", C.c_int32),
-        ("q", C.c_void_p), ("q_row_stride", C.c_int64), ("q_head_stride", C.c_int64), ("k_min", C.c_void_p), ("k_max", C.c_void_p),
-        ("page_table", C.c_void_p), ("len", C.c_void_p), ("max_sel", C.c_int32), ("n_first", C.c_int32), ("n_last", C.c_int32),
-        ("max_len", C.c_int32), ("sel", C.c_void_p), ("n_sel", C.c_void_p), ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t),
-    ]
-
-
 _lib = None
 
 
@@ -157,13 +118,6 @@ def lib():
         L.cerb_gemm_scratch_bytes.argtypes = [C.c_int32] * 3 + [C.POINTER(C.c_size_t)]
         L.cerb_gemm.argtypes = [C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
                                 C.c_void_p, C.c_size_t, C.c_void_p]
-        L.cerb_pages_plan.argtypes = [C.POINTER(Pages), C.c_void_p, C.c_int32] + [C.c_void_p] * 6
-        L.cerb_pages_trim.argtypes = [C.POINTER(Pages), C.c_void_p, C.c_void_p]
-        L.cerb_kv_append.argtypes = [C.POINTER(KvAppendArgs), C.c_void_p]
-        L.cerb_paged_attention_scratch_bytes.argtypes = [C.c_int32] * 8 + [C.POINTER(C.c_size_t)]
-        L.cerb_paged_attention.argtypes = [C.POINTER(PagedAttnArgs), C.c_void_p]
-        L.cerb_page_select_scratch_bytes.argtypes = [C.c_int32] * 7 + [C.POINTER(C.c_size_t)]
-        L.cerb_page_select.argtypes = [C.POINTER(PageSelectArgs), C.c_void_p]
         L.cerb_gemm_plan.argtypes = [C.c_int32] * 4 + [C.c_void_p]
         L.cerb_read_state.argtypes = [C.c_void_p] * 5
         L.cerb_device_status.argtypes = [C.c_void_p, C.c_void_p]
@@ -534,36 +488,7 @@ def gemm(X: torch.Tensor, W: torch.Tensor, scratch: Optional[torch.Tensor] = Non
     return out
 
 
-# ---- paged-cache operators of a serving loop (see the section on them in cerb.h)
-
-
-def _refuse(what: str, why: str, code: int = E_ARG):
-    e = CerbError(code, what)
-    e.args = ("%s: %s" % (e.args[0], why),)
-    raise e
-
-
-# (a call's checks are written for their cost: an attribute of a tensor is 0.06 to 0.2 us, and a step makes several calls a layer)
-def _index_tensors(what: str, device: int, tensors) -> None:
-    """Lengths, tables, lists and counts: int32, in one piece, on that GPU."""
-    if device < 0:
-        _refuse(what, "tensors must be on a GPU")
-    for t in tensors:
-        if t.dtype is not torch.int32 or not t.is_contiguous():
-            _refuse(what, "lengths, tables, lists and counts are contiguous int32 tensors")
-        if t.get_device() != device:
-            _refuse(what, "tensors are on different devices")
-
-
-def _call(fn, what: str, device: int, *args) -> None:
-    """On the tensors' own device, and the stream that is current there."""
-    if device == torch.cuda.current_device():
-        rc = fn(*args, _stream())
-    else:
-        with torch.cuda.device(device):
-            rc = fn(*args, _stream())
-    if rc != OK:
-        raise CerbError(rc, what)
+# ---- paged-cache operators of a serving loop (see the section on them in cerb.h); arguments are checked and outputs made in csrc/paged_binding.cpp
 
 
 class PagePlan(NamedTuple):
@@ -574,142 +499,49 @@ class PagePlan(NamedTuple):
     granted: torch.Tensor        # [B] tokens that a request got room for: all it wanted, or 0
 
 
-def _pages(what: str, device: int, n: torch.Tensor, lens, page_table, free_pages, n_free) -> Pages:
-    _index_tensors(what, device, (n, lens, page_table, free_pages, n_free))
-    B = lens.numel()
-    table = page_table.shape
-    if lens.dim() != 1 or n.shape != lens.shape or len(table) != 2 or table[0] != B or table[1] < 1 or free_pages.dim() != 1 or n_free.numel() != 1:
-        _refuse(what, "lens [B], a number a request, page_table [B][one column at least], free_pages [capacity], n_free [1]")
-    return Pages(B, table[1], free_pages.numel(), lens.data_ptr(), page_table.data_ptr(), free_pages.data_ptr(), n_free.data_ptr())
+_native = None
+
+
+def _paged():
+    """The native part of the binding; raises if it is missing (no fallback exists)."""
+    global _native
+    if _native is None:
+        try:
+            from . import _paged as native
+        except ImportError as e:
+            raise ImportError("the native part of the binding is missing: build it with `python -m paper_2410_13344_b200.build` (%s)" % e)
+        L = lib()
+        functions = ("cerb_pages_plan", "cerb_pages_trim", "cerb_kv_append", "cerb_paged_attention_scratch_bytes", "cerb_paged_attention",
+                     "cerb_page_select_scratch_bytes", "cerb_page_select")
+        native.setup(CerbError, PagePlan, [C.cast(getattr(L, f), C.c_void_p).value for f in functions])
+        _native = native
+    return _native
 
 
 def pages_plan(n_new: torch.Tensor, lens: torch.Tensor, page_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor,
                rows: int) -> PagePlan:
     """Room for n_new[b] more tokens of every request, in place: lens, page_table, free_pages and n_free are the state of the cache
     (see cerb_pages_plan); `rows` rows of a step's buffers describe the new tokens."""
-    what, device = "cerb_pages_plan", lens.get_device()
-    a = _pages(what, device, n_new, lens, page_table, free_pages, n_free)
-    B = a.B
-    if rows < 0:
-        _refuse(what, "rows is negative")
-    if B > 8192 or rows > 1 << 30:                           # (ahead of the allocation)
-        _refuse(what, "more than 8192 requests or 2^30 rows", E_SHAPE)
-    out = torch.empty(3 * rows + 2 * B + 1, dtype=torch.int32, device=lens.device)
-    at = out.data_ptr()
-    _call(lib().cerb_pages_plan, what, device, C.byref(a), n_new.data_ptr(), rows, at, at + 4 * rows, at + 8 * rows, at + 12 * rows,
-          at + 12 * rows + 4 * (B + 1))
-    return PagePlan(*out.split((rows, rows, rows, B + 1, B)))
+    return (_native or _paged()).pages_plan(n_new, lens, page_table, free_pages, n_free, rows)
 
 
 def pages_trim(keep: torch.Tensor, lens: torch.Tensor, page_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor) -> None:
     """Cuts every request down to keep[b] tokens and gives its other pages back, in place (see cerb_pages_trim)."""
-    device = lens.get_device()
-    a = _pages("cerb_pages_trim", device, keep, lens, page_table, free_pages, n_free)
-    _call(lib().cerb_pages_trim, "cerb_pages_trim", device, C.byref(a), keep.data_ptr())
-
-
-_DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
-
-
-def _pair(what: str, names: str, a: torch.Tensor, b: torch.Tensor, dims: int) -> int:
-    """dtype code of two tensors of a cache, alike and contiguous."""
-    if a.dim() != dims or a.shape != b.shape or not a.is_contiguous() or not b.is_contiguous():
-        _refuse(what, names + " (alike, contiguous)")
-    dt = a.dtype
-    if dt not in _DTYPES or b.dtype is not dt:
-        _refuse(what, "bfloat16 or float32, and no mixture")
-    if a.get_device() != b.get_device():
-        _refuse(what, "tensors are on different devices")
-    return _DTYPES[dt]
-
-
-_POOLS = "pools are [pages][KV heads][16][head_dim]"
-_SUMMARIES = "k_min and k_max are [pages][KV heads][head_dim]"
-
-
-def _rows(what: str, name: str, t: torch.Tensor, rows: int, heads: int, head_dim: int, like: torch.Tensor, device: int):
-    """(row stride, head stride) of a [rows][heads][head_dim] operand."""
-    if t.shape != (rows, heads, head_dim) or t.dtype is not like.dtype or t.get_device() != device:
-        _refuse(what, "%s is [%d][%d][%d], of the cache's type and on its device" % (name, rows, heads, head_dim))
-    r, h, e = t.stride()
-    if e != 1:
-        _refuse(what, "the elements of a head of %s are next to one another" % name)
-    return r, h
+    (_native or _paged()).pages_trim(keep, lens, page_table, free_pages, n_free)
 
 
 def kv_append(k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor,
               k_min: Optional[torch.Tensor] = None, k_max: Optional[torch.Tensor] = None) -> None:
-    """Writes k and v [T][KV heads][head_dim] (views into a packed product will do) into their slots of the pools, and keeps the pages' minima and
-    maxima (see cerb_kv_append)."""
-    what, device = "cerb_kv_append", k_pool.get_device()
-    dt = _pair(what, _POOLS, k_pool, v_pool, 4)
-    n_pages, Hk, page, D = k_pool.shape
-    if page != PAGE:
-        _refuse(what, _POOLS)
-    _index_tensors(what, device, (slot,))
-    T = slot.numel()
-    kr, kh = _rows(what, "k", k, T, Hk, D, k_pool, device)
-    vr, vh = _rows(what, "v", v, T, Hk, D, k_pool, device)
-    lo = hi = None
-    if k_min is not None or k_max is not None:
-        if k_min is None or k_max is None:
-            _refuse(what, "k_min and k_max come together")
-        if _pair(what, _SUMMARIES, k_min, k_max, 3) != dt or k_min.shape != (n_pages, Hk, D) or k_min.get_device() != device:
-            _refuse(what, "k_min and k_max are of other pages than the pools, or of another type")
-        lo, hi = k_min.data_ptr(), k_max.data_ptr()
-    a = KvAppendArgs(dt, T, Hk, D, k.data_ptr(), v.data_ptr(), kr, kh, vr, vh, slot.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), lo, hi, n_pages)
-    _call(lib().cerb_kv_append, what, device, C.byref(a))
-
-
-def _queries(what: str, q: torch.Tensor, Hk: int, D: int, like: torch.Tensor, device: int, page_table, lens):
-    """(B, heads, row stride, head stride, columns of the page table)"""
-    shape, table = q.shape, page_table.shape
-    if len(shape) != 3 or Hk < 1 or shape[1] < 1 or shape[1] % Hk:
-        _refuse(what, "q is [B][heads][head_dim], its heads a multiple of the KV heads")
-    B, H = shape[0], shape[1]
-    if len(table) != 2 or table[0] != B or table[1] < 1 or lens.shape != (B,):
-        _refuse(what, "a length and a row of the page table for every sequence")
-    _index_tensors(what, device, (page_table, lens))
-    r, h = _rows(what, "q", q, B, H, D, like, device)
-    return B, H, r, h, table[1]
-
-
-def _scratch(what: str, given: Optional[torch.Tensor], need: int, device: int):
-    """(address, bytes, what keeps it alive) of the scratch."""
-    if given is None:
-        if not need:
-            return None, 0, None
-        given = torch.empty(need, dtype=torch.uint8, device=device)
-    elif given.get_device() != device or given.dtype is not torch.uint8 or not given.is_contiguous():
-        _refuse(what, "scratch is a contiguous uint8 tensor on the same device")
-    return given.data_ptr(), given.numel(), given
-
-
-@functools.lru_cache(maxsize=256)
-def _scratch_bytes(fn: str, *sizes: int) -> int:
-    """(a function of the sizes alone)"""
-    nb = C.c_size_t(0)
-    _check(getattr(lib(), fn)(*sizes, C.byref(nb)), fn)
-    return nb.value
+    """Writes k and v [T][KV heads][head_dim] (views into a packed product will do) into their slots of the pools [pages][KV heads][16][head_dim], and keeps
+    the pages' minima and maxima [pages][KV heads][head_dim] (see cerb_kv_append)."""
+    (_native or _paged()).kv_append(k, v, slot, k_pool, v_pool, k_min, k_max)
 
 
 def page_select(q: torch.Tensor, k_min: torch.Tensor, k_max: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor, n_pages: int, max_len: int,
                 n_first: int = 1, n_last: int = 1, scratch: Optional[torch.Tensor] = None):
     """The n_pages pages of every (sequence, KV head) that hold the largest upper bounds of q . k, the first n_first and the last n_last always among
     them (see cerb_page_select).  Returns (sel [B][KV heads][n_pages] ascending and -1 behind, n_sel [B])."""
-    what, device = "cerb_page_select", k_min.get_device()
-    dt = _pair(what, _SUMMARIES, k_min, k_max, 3)
-    P, Hk, D = k_min.shape
-    B, H, qr, qh, mp = _queries(what, q, Hk, D, k_min, device, page_table, lens)
-    if n_pages < 1 or n_first < 0 or n_last < 0 or max_len < 1:
-        _refuse(what, "counts are not negative, n_pages and max_len one at least")
-    at, size, scratch = _scratch(what, scratch, _scratch_bytes("cerb_page_select_scratch_bytes", dt, B, H, Hk, D, mp, max_len), device)
-    sel = torch.empty((B, Hk, n_pages), dtype=torch.int32, device=device)
-    n_sel = torch.empty(B, dtype=torch.int32, device=device)
-    a = PageSelectArgs(dt, B, H, Hk, D, mp, P, q.data_ptr(), qr, qh, k_min.data_ptr(), k_max.data_ptr(), page_table.data_ptr(), lens.data_ptr(), n_pages,
-                       n_first, n_last, max_len, sel.data_ptr(), n_sel.data_ptr(), at, size)
-    _call(lib().cerb_page_select, what, device, C.byref(a))
-    return sel, n_sel
+    return (_native or _paged()).page_select(q, k_min, k_max, page_table, lens, n_pages, max_len, n_first, n_last, scratch)
 
 
 def paged_attention(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor, scale: float,
@@ -717,27 +549,4 @@ def paged_attention(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor,
                     scratch: Optional[torch.Tensor] = None):
     """Attention of one new token per sequence, q [B][heads][head_dim] (a view into a packed product will do), over the paged cache, over its last
     `window` tokens, or over the pages of page_select's lists (see cerb_paged_attention).  Returns (out, lse)."""
-    what, device = "cerb_paged_attention", k_pool.get_device()
-    dt = _pair(what, _POOLS, k_pool, v_pool, 4)
-    n_pages, Hk, page, D = k_pool.shape
-    if page != PAGE:
-        _refuse(what, _POOLS)
-    B, H, qr, qh, mp = _queries(what, q, Hk, D, k_pool, device, page_table, lens)
-    if max_len < 1 or window < 0:
-        _refuse(what, "max_len is one at least, window not negative")
-    max_sel, sel_at, n_sel_at = 0, None, None
-    if sel is not None or n_sel is not None:
-        if sel is None or n_sel is None:
-            _refuse(what, "sel and n_sel come together")
-        _index_tensors(what, device, (sel, n_sel))
-        lists = sel.shape
-        if len(lists) != 3 or lists[0] != B or lists[1] != Hk or lists[2] < 1 or n_sel.shape != (B,):
-            _refuse(what, "sel is [B][KV heads][pages], n_sel [B]")
-        max_sel, sel_at, n_sel_at = lists[2], sel.data_ptr(), n_sel.data_ptr()
-    at, size, scratch = _scratch(what, scratch, _scratch_bytes("cerb_paged_attention_scratch_bytes", dt, B, H, Hk, D, max_len, window, max_sel), device)
-    out = torch.empty((B, H, D), dtype=q.dtype, device=device)
-    lse = torch.empty((B, H), dtype=torch.float32, device=device) if want_lse else None
-    a = PagedAttnArgs(dt, B, H, Hk, D, mp, n_pages, q.data_ptr(), qr, qh, k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(), lens.data_ptr(),
-                      sel_at, n_sel_at, max_sel, out.data_ptr(), _ptr(lse), scale, max_len, window, at, size)
-    _call(lib().cerb_paged_attention, what, device, C.byref(a))
-    return out, lse
+    return (_native or _paged()).paged_attention(q, k_pool, v_pool, page_table, lens, scale, max_len, window, sel, n_sel, want_lse, scratch)

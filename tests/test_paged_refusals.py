@@ -9,10 +9,61 @@ from paper_2410_13344_b200 import binding
 AT = 1 << 20
 
 
+class Pages(C.Structure):
+    _fields_ = [
+        ("B", C.c_int32), ("max_pages", C.c_int32), ("free_cap", C.c_int32),
+        ("len", C.c_void_p), ("page_table", C.c_void_p), ("free_pages", C.c_void_p), ("n_free", C.c_void_p),
+    ]
+
+
+class KvAppendArgs(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int32), ("T", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("k", C.c_void_p), ("v", C.c_void_p),
+        ("k_row_stride", C.c_int64), ("k_head_stride", C.c_int64), ("v_row_stride", C.c_int64), ("v_head_stride", C.c_int64),
+        ("slot", C.c_void_p), ("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("k_min", C.c_void_p), ("k_max", C.c_void_p),
+        ("n_pool_pages", C.c_int32),
+    ]
+
+
+class PagedAttnArgs(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int32), ("B", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("max_pages", C.c_int32), ("n_pool_pages", C.c_int32),
+        ("q", C.c_void_p), ("q_row_stride", C.c_int64), ("q_head_stride", C.c_int64), ("k_pool", C.c_void_p), ("v_pool", C.c_void_p),
+        ("page_table", C.c_void_p), ("len", C.c_void_p), ("sel", C.c_void_p), ("n_sel", C.c_void_p), ("max_sel", C.c_int32),
+        ("out", C.c_void_p), ("lse", C.c_void_p), ("scale", C.c_float), ("max_len", C.c_int32), ("window", C.c_int32),
+        ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t),
+    ]
+
+
+class PageSelectArgs(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int32), ("B", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("max_pages", C.c_int32), ("n_pool_pages", C.c_int32),
+        ("q", C.c_void_p), ("q_row_stride", C.c_int64), ("q_head_stride", C.c_int64), ("k_min", C.c_void_p), ("k_max", C.c_void_p),
+        ("page_table", C.c_void_p), ("len", C.c_void_p), ("max_sel", C.c_int32), ("n_first", C.c_int32), ("n_last", C.c_int32),
+        ("max_len", C.c_int32), ("sel", C.c_void_p), ("n_sel", C.c_void_p), ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t),
+    ]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def argument_types():
+    L = binding.lib()
+    L.cerb_pages_plan.argtypes = [C.POINTER(Pages), C.c_void_p, C.c_int32] + [C.c_void_p] * 6
+    L.cerb_pages_trim.argtypes = [C.POINTER(Pages), C.c_void_p, C.c_void_p]
+    L.cerb_kv_append.argtypes = [C.POINTER(KvAppendArgs), C.c_void_p]
+    L.cerb_paged_attention_scratch_bytes.argtypes = [C.c_int32] * 8 + [C.POINTER(C.c_size_t)]
+    L.cerb_paged_attention.argtypes = [C.POINTER(PagedAttnArgs), C.c_void_p]
+    L.cerb_page_select_scratch_bytes.argtypes = [C.c_int32] * 7 + [C.POINTER(C.c_size_t)]
+    L.cerb_page_select.argtypes = [C.POINTER(PageSelectArgs), C.c_void_p]
+
+
+
 def _pages(**kw):
     a = dict(B=4, max_pages=8, free_cap=32, len=AT, page_table=AT, free_pages=AT, n_free=AT)
     a.update(kw)
-    return binding.Pages(**a)
+    return Pages(**a)
 
 
 def test_pages_refusals():
@@ -42,7 +93,7 @@ def test_append_refusals():
         a = dict(dtype=binding.BF16, T=4, n_kv_heads=2, head_dim=64, k=AT, v=AT, k_row_stride=128, k_head_stride=64, v_row_stride=128, v_head_stride=64,
                  slot=AT, k_pool=AT, v_pool=AT, k_min=AT, k_max=AT, n_pool_pages=8)
         a.update(kw)
-        return L.cerb_kv_append(C.byref(binding.KvAppendArgs(**a)), None)
+        return L.cerb_kv_append(C.byref(KvAppendArgs(**a)), None)
 
     assert call(T=0) == binding.OK and call(T=0, k=None, v=None, slot=None) == binding.OK
     for name in ("k", "v", "slot", "k_pool", "v_pool", "k_min", "k_max"):
@@ -66,7 +117,7 @@ def test_attention_refusals():
                  k_pool=AT, v_pool=AT, page_table=AT, len=AT, sel=None, n_sel=None, max_sel=0, out=AT, lse=AT, scale=1.0, max_len=100, window=0,
                  scratch=None, scratch_bytes=0)
         a.update(kw)
-        return L.cerb_paged_attention(C.byref(binding.PagedAttnArgs(**a)), None)
+        return L.cerb_paged_attention(C.byref(PagedAttnArgs(**a)), None)
 
     none = dict(B=0, q=None, k_pool=None, v_pool=None, page_table=None, len=None, out=None)
     assert call(**none) == binding.OK
@@ -101,7 +152,7 @@ def test_select_refusals():
         a = dict(dtype=binding.BF16, B=1, n_heads=8, n_kv_heads=2, head_dim=64, max_pages=8, n_pool_pages=8, q=AT, q_row_stride=512, q_head_stride=64,
                  k_min=AT, k_max=AT, page_table=AT, len=AT, max_sel=4, n_first=1, n_last=1, max_len=100, sel=AT, n_sel=AT, scratch=None, scratch_bytes=0)
         a.update(kw)
-        return L.cerb_page_select(C.byref(binding.PageSelectArgs(**a)), None)
+        return L.cerb_page_select(C.byref(PageSelectArgs(**a)), None)
 
     assert call(B=0, q=None, k_min=None, k_max=None, page_table=None, len=None, sel=None, n_sel=None) == binding.OK
     for name in ("q", "k_min", "k_max", "page_table", "len", "sel", "n_sel"):
