@@ -20,10 +20,9 @@ namespace cerb {
 namespace {
 
 constexpr int SC_WARPS = 4;
-constexpr int SEL_THREADS = 512;
 constexpr int SEL_KEEP = 8192;              // scores that shared memory keeps: those of caches of up to so many pages
-constexpr int SEL_BINS = 512;
-constexpr int SEL_LIST = 1024;              // pages near the border that are ranked one against another
+constexpr int SEL_LIST = 512;               // pages near the border that are ranked one against another
+constexpr int kMaxChunks = 512;             // a thread of the selection for each
 constexpr int kMaxSelectPages = 1 << 17;    // (a bit mask of them lies in shared memory)
 
 // What a CTA that scores pages leaves behind, over those that are up for selection.
@@ -286,23 +285,21 @@ __global__ void __launch_bounds__(SC_WARPS * 32, 4) page_score_f32_kernel(const 
   leave_chunk<float>(p, unit, chunk, bound, least, most, odd);
 }
 
-// A page's score for one head in fp64, by eight lanes (all 32 of the warp call).
-template <typename T> __device__ __forceinline__ double wide(T x);
-template <> __device__ __forceinline__ double wide<float>(float x) { return (double)x; }
-template <> __device__ __forceinline__ double wide<bf16>(bf16 x) { return (double)__bfloat162float(x); }
+// A page's score for one head in fp64, by eight lanes (all 32 of the warp call).  `at`: where the page lies, -1: nowhere.
+template <typename T> __device__ __forceinline__ float wide(T x);
+template <> __device__ __forceinline__ float wide<float>(float x) { return x; }
+template <> __device__ __forceinline__ float wide<bf16>(bf16 x) { return __bfloat162float(x); }
 template <typename T, int DH>
-__device__ __forceinline__ double score_again(const SelectParams& p, int b, int kvh, int page, int head, int lane) {
+__device__ __forceinline__ double score_again(const SelectParams& p, int b, int kvh, int at, int head, int lane) {
   constexpr int E = 16 / sizeof(T);                                      // elements of a load
   struct alignas(16) Elems {
     T x[E];
   };
-  const int at = page_at(p, b, page);
+  constexpr int J = DH / (8 * E);
   const size_t from = ((size_t)max(at, 0) * p.Hk + kvh) * DH + lane % 8 * E;
   const T* hi = reinterpret_cast<const T*>(p.k_max) + from;
   const T* lo = reinterpret_cast<const T*>(p.k_min) + from;
   const T* q = reinterpret_cast<const T*>(p.q) + (size_t)b * p.q_row + (size_t)(kvh * p.G + head) * p.q_head + lane % 8 * E;
-  double s = 0.0;
-  constexpr int J = DH / (8 * E);
   Elems h[J], l[J], x[J];
 #pragma unroll
   for (int j = 0; j < J; ++j) {
@@ -310,13 +307,20 @@ __device__ __forceinline__ double score_again(const SelectParams& p, int b, int 
     l[j] = *reinterpret_cast<const Elems*>(lo + j * 8 * E);
     x[j] = *reinterpret_cast<const Elems*>(q + j * 8 * E);
   }
+  double sum[2] = {0.0, 0.0};
 #pragma unroll
   for (int j = 0; j < J; ++j)
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const double y = wide<T>(x[j].x[e]), a = y * wide<T>(l[j].x[e]), c = y * wide<T>(h[j].x[e]);
-      s += a != a || c != c ? a + c : fmax(a, c);
+      // the larger product is the one with kmax where q is positive, with kmin where it is negative; where q is zero, and where one of them is not a
+      // number, the one that makes the sum what the definition makes it
+      const float y = wide<T>(x[j].x[e]), c = wide<T>(h[j].x[e]), a = wide<T>(l[j].x[e]);
+      float k = y > 0.f || (y == 0.f && fabsf(c) >= fabsf(a)) ? c : a;
+      if (c != c) k = c;
+      if (a != a) k = a;
+      sum[e & 1] = fma((double)y, (double)k, sum[e & 1]);
     }
+  double s = sum[0] + sum[1];
 #pragma unroll
   for (int w = 4; w > 0; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
   return at < 0 ? -INFINITY : s;
@@ -335,6 +339,7 @@ __device__ __forceinline__ unsigned long long ordered(double x) {
   return i >> 63 ? ~i : i | 0x8000000000000000ull;
 }
 
+template <int SEL_THREADS>
 __device__ __forceinline__ int block_sum(int v, int* red) {
   constexpr int WARPS = SEL_THREADS / 32;
   const int lane = threadIdx.x & 31;
@@ -344,6 +349,7 @@ __device__ __forceinline__ int block_sum(int v, int* red) {
   __syncthreads();
   return __reduce_add_sync(0xffffffffu, lane < WARPS ? red[lane] : 0);
 }
+template <int SEL_THREADS>
 __device__ __forceinline__ int block_scan(int v, int* red, int& total) {     // exclusive
   constexpr int WARPS = SEL_THREADS / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -372,14 +378,15 @@ __device__ __forceinline__ int block_scan(int v, int* red, int& total) {     // 
 // what lies within 2 E of them, are ranked in fp64.  Scores of up to SEL_KEEP pages stay in shared memory, those of more are read again at every pass.
 // With a CTA to an SM, each of its instructions executed a few times, much of the time is that of fetching them: the loops stay rolled.  (Unrolled, with
 // the scores in registers, the histogram of 2000 pages took as long as that of 8192, 3 us.)
-template <typename T, int DH>
-__global__ void __launch_bounds__(SEL_THREADS, 2) page_select_kernel(const SelectParams p) {
+template <typename T, int DH, int SEL_THREADS>
+__global__ void __launch_bounds__(SEL_THREADS, 1024 / SEL_THREADS) page_select_kernel(const SelectParams p) {
+  constexpr int SEL_BINS = SEL_THREADS;
   __shared__ int red[32], hist[SEL_BINS];
-  __shared__ unsigned taken[kMaxSelectPages / 32];
-  __shared__ int list[SEL_LIST];
+  __shared__ int list[SEL_LIST], list_at[SEL_LIST];
   __shared__ unsigned long long again[SEL_LIST];
   __shared__ int s_lo, s_hi, s_n, s_bin, s_above, s_bound, s_odd;
-  extern __shared__ float kept[];
+  extern __shared__ unsigned taken[];                                    // a bit for each page of the table's row, then the scores that are kept
+  float* kept = reinterpret_cast<float*>(taken + (p.max_pages + 31) / 32);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int unit = blockIdx.x, kvh = unit % p.Hk, b = unit / p.Hk;
   if (tid == 0) {
@@ -464,10 +471,9 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) page_select_kernel(const Selec
       });
       __syncthreads();
       // the bin with the want-th best: thread i looks at the i-th bin from above
-      static_assert(SEL_BINS == SEL_THREADS, "a bin per thread");
       const int mine = hist[SEL_BINS - 1 - tid];
       int total;
-      const int before = above + block_scan(mine, red, total);
+      const int before = above + block_scan<SEL_THREADS>(mine, red, total);
       if (before < want && before + mine >= want) { s_bin = SEL_BINS - 1 - tid; s_above = before; s_lo = ordered(INFINITY); s_hi = ordered(-INFINITY); }
       __syncthreads();
       const int bin = s_bin, count = hist[bin];
@@ -504,27 +510,34 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) page_select_kernel(const Selec
         ++sure;
       } else if (all_again || s >= t_lo) {
         const int at = atomicAdd(&s_n, 1);
-        if (at < SEL_LIST) { list[at] = i; again[at] = 0; }
+        if (at < SEL_LIST) { list[at] = i; list_at[at] = page_at(p, b, i); again[at] = 0; }
       }
     });
-  sure = block_sum(sure, red);
+  sure = block_sum<SEL_THREADS>(sure, red);
   const int near = s_n, rest = want - sure;
   if (near <= SEL_LIST) {
     if (near > rest) {
 #pragma unroll 1
       for (int i0 = warp * 4; i0 < near * p.G; i0 += SEL_THREADS / 8) {
         const int i = i0 + lane / 8, w = min(i, near * p.G - 1);
-        const double s = score_again<T, DH>(p, b, kvh, list[w / p.G], w % p.G, lane);
+        const double s = score_again<T, DH>(p, b, kvh, list_at[w / p.G], w % p.G, lane);
         if (lane % 8 == 0 && i == w) atomicMax(&again[w / p.G], ordered(s));
       }
       __syncthreads();
     }
-    for (int i = tid; i < near; i += SEL_THREADS) {
-      int rank = 0;
-      if (near > rest)
+    // a page's rank among them, by a warp
 #pragma unroll 1
-        for (int j = 0; j < near; ++j) rank += again[j] > again[i] || (again[j] == again[i] && list[j] < list[i]);
-      if (rank < rest) atomicOr(&taken[list[i] >> 5], 1u << (list[i] & 31));
+    for (int i = warp; i < near; i += SEL_THREADS / 32) {
+      int rank = 0;
+      if (near > rest) {
+        const unsigned long long mine = again[i];
+        const int page = list[i];
+        for (int j = lane; j - lane < near; j += 32) {
+          const unsigned long long other = j < near ? again[j] : 0;
+          rank += __popc(__ballot_sync(0xffffffffu, other > mine || (other == mine && j < near && list[j] < page)));
+        }
+      }
+      if (lane == 0 && rank < rest) atomicOr(&taken[list[i] >> 5], 1u << (list[i] & 31));
     }
   } else {
     // many near the border (a cache of equal keys, scores that are not finite): all of them in fp64, the border by bisection of the ordered values
@@ -532,10 +545,10 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) page_select_kernel(const Selec
     auto is_near = [&](int i) { return all_again || (score[i] >= t_lo && score[i] <= t_hi); };
 #pragma unroll 1
     for (int i0 = first + warp * 4; i0 < last; i0 += SEL_THREADS / 8) {
-      const int i = min(i0 + lane / 8, last - 1);
+      const int i = min(i0 + lane / 8, last - 1), at = page_at(p, b, i);
       unsigned long long best = 0;
 #pragma unroll 1
-      for (int h = 0; h < p.G; ++h) best = max(best, ordered(score_again<T, DH>(p, b, kvh, i, h, lane)));
+      for (int h = 0; h < p.G; ++h) best = max(best, ordered(score_again<T, DH>(p, b, kvh, at, h, lane)));
       if (lane % 8 == 0) far[i] = best;
     }
     __syncthreads();
@@ -545,7 +558,7 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) page_select_kernel(const Selec
       int cnt = 0;
 #pragma unroll 4
       for (int i = first + tid; i < last; i += SEL_THREADS) cnt += is_near(i) && far[i] >= c;
-      if (block_sum(cnt, red) >= rest) v = c;
+      if (block_sum<SEL_THREADS>(cnt, red) >= rest) v = c;
     }
     int over = 0;
     for (int i = first + tid; i < last; i += SEL_THREADS)
@@ -553,12 +566,12 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) page_select_kernel(const Selec
         atomicOr(&taken[i >> 5], 1u << (i & 31));
         ++over;
       }
-    int ties = rest - block_sum(over, red);
+    int ties = rest - block_sum<SEL_THREADS>(over, red);
     for (int i0 = first; i0 < last && ties > 0; i0 += SEL_THREADS) {
       const int i = i0 + tid;
       const int tie = i < last && is_near(i) && far[i] == v;
       int total;
-      const int before = block_scan(tie, red, total);
+      const int before = block_scan<SEL_THREADS>(tie, red, total);
       if (tie && before < ties) atomicOr(&taken[i >> 5], 1u << (i & 31));
       ties -= total;
     }
@@ -567,7 +580,7 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) page_select_kernel(const Selec
   int written = 0;
   for (int w0 = 0; w0 < words; w0 += SEL_THREADS) {
     unsigned m = w0 + tid < words ? taken[w0 + tid] : 0;
-    int total, at = written + block_scan(__popc(m), red, total);
+    int total, at = written + block_scan<SEL_THREADS>(__popc(m), red, total);
     for (; m; m &= m - 1) sel[at++] = (w0 + tid) * 32 + __ffs(m) - 1;
     written += total;
   }
@@ -581,11 +594,19 @@ int plan_select(int dtype, int B, int H, int Hk, int head_dim, int max_pages, si
   // as many CTAs as run at once, of no less than a round of their warps
   const int held = (int)(((long long)max_len + CERB_PAGE - 1) / CERB_PAGE), per = (dtype == CERB_BF16 ? 16 : 8) * SC_WARPS;
   const long long most = (std::min(held, max_pages) + per - 1) / per, want = units ? 148 * (dtype == CERB_BF16 ? 3 : 4) / units : 1;
-  *chunks = (int)std::max(1ll, std::min({most, want, (long long)SEL_THREADS}));
+  *chunks = (int)std::max(1ll, std::min({most, want, (long long)kMaxChunks}));
   *score_bytes = ((size_t)units * max_pages * sizeof(float) + 255) & ~(size_t)255;
   *bound_bytes = ((size_t)units * *chunks * sizeof(ChunkScores) + 255) & ~(size_t)255;
   *again_bytes = (size_t)units * max_pages * sizeof(unsigned long long);
   return CERB_OK;
+}
+
+template <typename T, int DH, int THREADS>
+int launch_select(const SelectParams& p, unsigned units, size_t smem, cudaStream_t st) {
+  auto kern = page_select_kernel<T, DH, THREADS>;
+  static std::atomic<uint64_t> done{0};
+  CERB_TRY(allow_smem(kern, done, kMaxSelectPages / 8 + SEL_KEEP * (int)sizeof(float)));
+  return launch_pdl(kern, dim3(units), dim3(THREADS), smem, st, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
 }
 
 }  // namespace
@@ -648,10 +669,13 @@ int cerb_page_select(const cerb_page_select_args* a, void* stream) {
   auto score = bf ? (big ? page_score_bf16_kernel<128> : page_score_bf16_kernel<64>) : (big ? page_score_f32_kernel<128> : page_score_f32_kernel<64>);
   const size_t q_smem = bf ? (size_t)(p.G + 7) / 8 * 8 * (a->head_dim + 8) * sizeof(bf16) : (size_t)p.G * a->head_dim * sizeof(float);
   if (launch_pdl(score, dim3(units * (unsigned)chunks), dim3(SC_WARPS * 32), q_smem, st, p) != cudaSuccess) return CERB_E_CUDA;
-  auto kern = bf ? (big ? page_select_kernel<bf16, 128> : page_select_kernel<bf16, 64>) : (big ? page_select_kernel<float, 128> : page_select_kernel<float, 64>);
-  static std::atomic<uint64_t> done[4];
-  CERB_TRY(allow_smem(kern, done[2 * bf + big], SEL_KEEP * (int)sizeof(float)));
-  return launch_pdl(kern, dim3(units), dim3(SEL_THREADS), std::min(a->max_pages, SEL_KEEP) * sizeof(float), st, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
+  const size_t smem = ((size_t)a->max_pages + 31) / 32 * sizeof(unsigned) + std::min(a->max_pages, SEL_KEEP) * sizeof(float);
+  // (twice the threads while every unit has an SM to itself)
+  if (units <= 148)
+    return bf ? (big ? launch_select<bf16, 128, 1024>(p, units, smem, st) : launch_select<bf16, 64, 1024>(p, units, smem, st))
+              : (big ? launch_select<float, 128, 1024>(p, units, smem, st) : launch_select<float, 64, 1024>(p, units, smem, st));
+  return bf ? (big ? launch_select<bf16, 128, 512>(p, units, smem, st) : launch_select<bf16, 64, 512>(p, units, smem, st))
+            : (big ? launch_select<float, 128, 512>(p, units, smem, st) : launch_select<float, 64, 512>(p, units, smem, st));
 }
 
 }  // extern "C"
