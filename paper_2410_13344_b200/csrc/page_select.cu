@@ -22,25 +22,25 @@ namespace {
 constexpr int SC_WARPS = 4;
 constexpr int SEL_KEEP = 8192;              // scores that shared memory keeps: those of caches of up to so many pages
 constexpr int SEL_LIST = 512;               // pages near the border that are ranked one against another
-constexpr int kMaxChunks = 512;             // a thread of the selection for each
 constexpr int kMaxSelectPages = 1 << 17;    // (a bit mask of them lies in shared memory)
 
-// What a CTA that scores pages leaves behind, over those that are up for selection.
-struct ChunkScores {
+// What is known of the scores of a tile of pages (of those of it that are up for selection).
+struct TileScores {
   float bound;                 // of the error of its scores
   float lo, hi;                // smallest and largest score
   int odd;                     // scores that are not finite
 };
+constexpr int kTile = 16;      // pages
 
 struct SelectParams {
   const void *q, *k_min, *k_max;
   const int32_t *page_table, *len;
   int32_t *sel, *n_sel;
   float* score;                // [unit][max_pages]
-  ChunkScores* chunk;          // [unit][chunks]
+  TileScores* tile;            // [unit][tiles]
   unsigned long long* again;   // [unit][max_pages]: scores of 64 bits as ordered whole numbers
   long long q_row, q_head;     // elements
-  int B, H, Hk, G, max_pages, n_pool_pages, K, n_first, n_last, chunks;
+  int B, H, Hk, G, max_pages, n_pool_pages, K, n_first, n_last, tiles;
 };
 
 __device__ __forceinline__ int pages_held(const SelectParams& p, int b) {
@@ -71,11 +71,8 @@ template <typename T> __device__ __forceinline__ float error_factor();
 template <> __device__ __forceinline__ float error_factor<bf16>() { return 2.1579186e-5f; }
 template <> __device__ __forceinline__ float error_factor<float>() { return 1.0f / 524288; }
 
-// What is known of a CTA's scores, from what its threads know.
-template <typename T>
-__device__ __forceinline__ void leave_chunk(const SelectParams& p, int unit, int chunk, float bound, float lo, float hi, bool odd) {
-  __shared__ ChunkScores s_c[SC_WARPS];
-  const int warp = threadIdx.x >> 5;
+// Leaves what a warp's lanes know of a tile.
+__device__ __forceinline__ void leave_tile(TileScores* to, float bound, float lo, float hi, bool odd) {
 #pragma unroll
   for (int w = 1; w < 32; w <<= 1) {
     bound = fmaxf(bound, __shfl_xor_sync(0xffffffffu, bound, w));
@@ -83,90 +80,98 @@ __device__ __forceinline__ void leave_chunk(const SelectParams& p, int unit, int
     hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, w));
   }
   odd = __any_sync(0xffffffffu, odd);
-  if ((threadIdx.x & 31) == 0) s_c[warp] = ChunkScores{bound, lo, hi, odd};
-  __syncthreads();
-  if (threadIdx.x) return;
-  ChunkScores c = s_c[0];
-  for (int w = 1; w < SC_WARPS; ++w) {
-    c.bound = fmaxf(c.bound, s_c[w].bound);
-    c.lo = fminf(c.lo, s_c[w].lo);
-    c.hi = fmaxf(c.hi, s_c[w].hi);
-    c.odd |= s_c[w].odd;
-  }
-  c.bound *= error_factor<T>();
-  p.chunk[(size_t)unit * p.chunks + chunk] = c;
+  if ((threadIdx.x & 31) == 0) *reinterpret_cast<float4*>(to) = make_float4(bound, lo, hi, __int_as_float(odd));
+}
+
+// A warp's way through its share of the tiles of all units whose pages have to be selected from.
+struct TileWalk {
+  int b, kvh, tile, N, tiles;  // of the present one: sequence, KV head, tile, the sequence's pages and tiles
+  long long left;              // with the present one
+};
+__device__ __forceinline__ int tiles_of(const SelectParams& p, int b) {
+  const int N = pages_held(p, b);
+  return N > p.K ? (N + kTile - 1) / kTile : 0;
+}
+__device__ __forceinline__ TileWalk walk_tiles(const SelectParams& p) {
+  const Share s = share_of(p.B, [&](int b) { return (long long)tiles_of(p, b) * p.Hk; }, blockIdx.x * SC_WARPS + (threadIdx.x >> 5), gridDim.x * SC_WARPS, 1);
+  TileWalk w;
+  w.left = s.end - s.begin;
+  w.b = s.b;
+  if (w.left <= 0) return w;
+  w.N = pages_held(p, w.b);
+  w.tiles = tiles_of(p, w.b);
+  w.kvh = (int)((unsigned)s.off / (unsigned)w.tiles);                    // (less than 2^31: a sequence has 2^13 tiles at most, and 2^16 KV heads)
+  w.tile = (int)((unsigned)s.off - (unsigned)w.kvh * w.tiles);
+  return w;
+}
+__device__ __forceinline__ void next_tile(const SelectParams& p, TileWalk& w) {
+  if (--w.left <= 0 || ++w.tile < w.tiles) return;
+  w.tile = 0;
+  if (++w.kvh < p.Hk) return;
+  w.kvh = 0;
+  do w.tiles = tiles_of(p, ++w.b);
+  while (w.tiles == 0);
+  w.N = pages_held(p, w.b);
 }
 
 // bf16 scores: 16 pages on the rows of a warp MMA, eight heads on its columns, kmax and kmin straight from global memory in the order in which the lanes
 // load them, the next 16 pages' on their way.  S is a product like the scores, of absolute values.
 template <int DH>
 __global__ void __launch_bounds__(SC_WARPS * 32, 3) page_score_bf16_kernel(const SelectParams p) {
-  constexpr int KC = DH / 32, LD = DH + 8;
-  extern __shared__ __align__(16) bf16 q_s[];                            // [heads padded to 8][LD]
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int chunk = blockIdx.x % p.chunks, unit = blockIdx.x / p.chunks, kvh = unit % p.Hk, b = unit / p.Hk;
+  constexpr int KC = DH / 32;
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   griddep_wait();
   griddep_launch();
-  const int step = p.chunks * SC_WARPS;
-  const bf16* src_hi = reinterpret_cast<const bf16*>(p.k_max) + (size_t)kvh * DH + 8 * t;
-  const bf16* src_lo = reinterpret_cast<const bf16*>(p.k_min) + (size_t)kvh * DH + 8 * t;
+  TileWalk now = walk_tiles(p);
   struct Pages {
     int at[2];
   };
-  auto find = [&](int r) {
+  auto find = [&](const TileWalk& w) {
     Pages x;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int page = r * 16 + g + 8 * e;
-      x.at[e] = page < p.max_pages ? page_at(p, b, page) : -1;           // (of the table's row: the length is still on its way)
+      const int page = w.tile * kTile + g + 8 * e;
+      x.at[e] = w.left > 0 && page < w.N ? page_at(p, w.b, page) : -1;
     }
     return x;
   };
-  auto load = [&](uint4 (&x)[2][KC], const bf16* src, const Pages& w) {
+  auto load = [&](uint4 (&x)[2][KC], const void* from, const TileWalk& w, const Pages& pages) {
+    const bf16* src = reinterpret_cast<const bf16*>(from) + (size_t)w.kvh * DH + 8 * t;
 #pragma unroll
     for (int e = 0; e < 2; ++e)
 #pragma unroll
       for (int j = 0; j < KC; ++j) {
         x[e][j] = make_uint4(0, 0, 0, 0);
-        if (w.at[e] >= 0) x[e][j] = ld16(src + (size_t)w.at[e] * p.Hk * DH + 32 * j);
+        if (pages.at[e] >= 0) x[e][j] = ld16(src + (size_t)pages.at[e] * p.Hk * DH + 32 * j);
       }
   };
-  uint4 hi[2][KC], lo[2][KC];
-  int r = chunk * SC_WARPS + warp;
-  Pages now = find(r), then = find(r + step);
-  const int N = pages_held(p, b);
-  if (N <= p.K) return;                                                  // all of them
+  uint4 hi[2][KC], lo[2][KC], q[KC];
+  TileWalk then = now;
+  if (then.left > 0) next_tile(p, then);
+  Pages pages = find(now), pages_then = find(then);
+  load(hi, p.k_max, now, pages);
+  load(lo, p.k_min, now, pages);
   const int tiles = (p.G + 7) / 8;
-  for (int i = threadIdx.x; i < tiles * 8 * (DH / 8); i += SC_WARPS * 32) {
-    const int h = i / (DH / 8), c = i % (DH / 8) * 8;
-    *reinterpret_cast<uint4*>(q_s + h * LD + c) =
-        h < p.G ? *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(p.q) + (size_t)b * p.q_row + (size_t)(kvh * p.G + h) * p.q_head + c)
-                : make_uint4(0, 0, 0, 0);
-  }
-  // (pages behind the last are read as if there were none: stale entries of the table may name any)
-  auto live = [&](Pages& w, int at) {
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-      if (at * 16 + g + 8 * e >= N) w.at[e] = -1;
-  };
-  live(now, r);
-  live(then, r + step);
-  load(hi, src_hi, now);
-  load(lo, src_lo, now);
-  __syncthreads();
-  float bound = 0.f, least = INFINITY, most = -INFINITY;
-  bool odd = false;
-  for (; r * 16 < N; r += step) {
-    float best[2] = {-INFINITY, -INFINITY};
+  int have = -1;                                                         // the (sequence, KV head) of the queries that are in q, where they all fit
+  while (now.left > 0) {
+    TileWalk after = then;
+    if (after.left > 0) next_tile(p, after);
+    const Pages pages_after = find(after);
+    const int unit = now.b * p.Hk + now.kvh;
+    float best[2] = {-INFINITY, -INFINITY}, bound = 0.f;
     bool nan[2] = {false, false};
-    Pages after = find(r + 2 * step);
     for (int n = 0; n < tiles; ++n) {
+      if (tiles > 1 || unit != have) {
+        have = unit;
+        const bf16* src = reinterpret_cast<const bf16*>(p.q) + (size_t)now.b * p.q_row + (size_t)(now.kvh * p.G + 8 * n + g) * p.q_head + 8 * t;
+#pragma unroll
+        for (int j = 0; j < KC; ++j) q[j] = 8 * n + g < p.G ? *reinterpret_cast<const uint4*>(src + 32 * j) : make_uint4(0, 0, 0, 0);
+      }
       float sh[4] = {0.f, 0.f, 0.f, 0.f}, sl[4] = {0.f, 0.f, 0.f, 0.f}, bh[4] = {0.f, 0.f, 0.f, 0.f}, bl[4] = {0.f, 0.f, 0.f, 0.f};
       auto multiply = [&](const uint4 (&x)[2][KC], bool up, float (&s)[4], float (&a)[4]) {
 #pragma unroll
         for (int j = 0; j < KC; ++j) {
-          const uint4 qv = *reinterpret_cast<const uint4*>(q_s + (8 * n + g) * LD + 32 * j + 8 * t);
-          const uint32_t qw[4] = {qv.x, qv.y, qv.z, qv.w};
+          const uint32_t qw[4] = {q[j].x, q[j].y, q[j].z, q[j].w};
           const uint32_t x0[4] = {x[0][j].x, x[0][j].y, x[0][j].z, x[0][j].w}, x1[4] = {x[1][j].x, x[1][j].y, x[1][j].z, x[1][j].w};
 #pragma unroll
           for (int w = 0; w < 4; w += 2) {
@@ -177,18 +182,20 @@ __global__ void __launch_bounds__(SC_WARPS * 32, 3) page_score_bf16_kernel(const
         }
       };
       multiply(hi, true, sh, bh);
-      if (n == tiles - 1) load(hi, src_hi, then);
+      if (n == tiles - 1) load(hi, p.k_max, then, pages_then);
       multiply(lo, false, sl, bl);
-      if (n == tiles - 1) load(lo, src_lo, then);
+      if (n == tiles - 1) load(lo, p.k_min, then, pages_then);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (8 * n + 2 * t + (e & 1) >= p.G) continue;
         const float s = sh[e] + sl[e], a = bh[e] + bl[e];
         nan[e >> 1] |= s != s;
         best[e >> 1] = fmaxf(best[e >> 1], s);
-        if (now.at[e >> 1] >= 0) bound = a == a ? fmaxf(bound, a) : INFINITY;
+        if (pages.at[e >> 1] >= 0) bound = a == a ? fmaxf(bound, a) : INFINITY;
       }
     }
+    float least = INFINITY, most = -INFINITY;
+    bool odd = false;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       float s = nan[e] ? NAN : best[e];
@@ -197,92 +204,91 @@ __global__ void __launch_bounds__(SC_WARPS * 32, 3) page_score_bf16_kernel(const
         const float other = __shfl_xor_sync(0xffffffffu, s, w);
         s = s != s || other != other ? NAN : fmaxf(s, other);
       }
-      const int page = r * 16 + g + 8 * e;
-      if (now.at[e] < 0) s = -INFINITY;                                  // (a page that lies nowhere: below every other)
-      if (page < N) {
+      const int page = now.tile * kTile + g + 8 * e;
+      if (pages.at[e] < 0) s = -INFINITY;                                // (a page that lies nowhere: below every other)
+      if (page < now.N) {
         if (t == 0) p.score[(size_t)unit * p.max_pages + page] = s;
-        if (page >= p.n_first && page < N - p.n_last) {
+        if (page >= p.n_first && page < now.N - p.n_last) {
           odd |= !(fabsf(s) < INFINITY);
           least = fminf(least, s);
           most = fmaxf(most, s);
         }
       }
     }
+    leave_tile(p.tile + (size_t)unit * p.tiles + now.tile, bound * error_factor<bf16>(), least, most, odd);
     now = then;
-    live(after, r + 2 * step);
+    pages = pages_then;
     then = after;
+    pages_then = pages_after;
   }
-  leave_chunk<bf16>(p, unit, chunk, bound, least, most, odd);
 }
 
-// fp32 scores: eight pages to a warp at a time, DH / 32 elements to a lane; the scores of a head and their S are 16 sums over the lanes.
+// fp32 scores: half a tile to a warp at a time, DH / 32 elements to a lane; the scores of a head and their S are 16 sums over the lanes.
 template <int DH>
 __global__ void __launch_bounds__(SC_WARPS * 32, 4) page_score_f32_kernel(const SelectParams p) {
   constexpr int E = DH / 32, PAGES = 8;
   struct alignas(4 * E) Elems {
     float x[E];
   };
-  extern __shared__ __align__(16) float qf_s[];                          // [heads][DH]
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int chunk = blockIdx.x % p.chunks, unit = blockIdx.x / p.chunks, kvh = unit % p.Hk, b = unit / p.Hk;
+  const int lane = threadIdx.x & 31;
   griddep_wait();
   griddep_launch();
-  const int N = pages_held(p, b);
-  if (N <= p.K) return;
-  for (int i = threadIdx.x; i < p.G * DH; i += SC_WARPS * 32)
-    qf_s[i] = reinterpret_cast<const float*>(p.q)[(size_t)b * p.q_row + (size_t)(kvh * p.G + i / DH) * p.q_head + i % DH];
-  __syncthreads();
-  const Elems* src_hi = reinterpret_cast<const Elems*>(p.k_max) + (size_t)kvh * 32 + lane;
-  const Elems* src_lo = reinterpret_cast<const Elems*>(p.k_min) + (size_t)kvh * 32 + lane;
-  float bound = 0.f, least = INFINITY, most = -INFINITY;
-  bool odd = false;
-  for (int page0 = (chunk * SC_WARPS + warp) * PAGES; page0 < N; page0 += p.chunks * SC_WARPS * PAGES) {
-    const int mine = page0 + lane < N && lane < PAGES ? page_at(p, b, page0 + lane) : -1;
-    Elems hi[PAGES], lo[PAGES];
-#pragma unroll
-    for (int j = 0; j < PAGES; ++j) {
-      const int at = __shfl_sync(0xffffffffu, mine, j);
-#pragma unroll
-      for (int e = 0; e < E; ++e) hi[j].x[e] = lo[j].x[e] = 0.f;
-      if (at >= 0) {
-        hi[j] = src_hi[(size_t)at * p.Hk * 32];
-        lo[j] = src_lo[(size_t)at * p.Hk * 32];
-      }
-    }
-    float best = -INFINITY, far = 0.f;                                   // lanes 0 .. 15: score of page lane / 2; the others: S of page (lane - 16) / 2
-    bool nan = false;
-    for (int h = 0; h < p.G; ++h) {
-      const Elems x = *reinterpret_cast<const Elems*>(qf_s + h * DH + lane * E);
-      float s[2 * PAGES];
+  for (TileWalk now = walk_tiles(p); now.left > 0; next_tile(p, now)) {
+    const int unit = now.b * p.Hk + now.kvh;
+    const Elems* src_hi = reinterpret_cast<const Elems*>(p.k_max) + (size_t)now.kvh * 32 + lane;
+    const Elems* src_lo = reinterpret_cast<const Elems*>(p.k_min) + (size_t)now.kvh * 32 + lane;
+    const float* src_q = reinterpret_cast<const float*>(p.q) + (size_t)now.b * p.q_row + (size_t)now.kvh * p.G * p.q_head + lane * E;
+    float bound = 0.f, least = INFINITY, most = -INFINITY;
+    bool odd = false;
+    const int of_tile = lane < kTile && now.tile * kTile + lane < now.N ? page_at(p, now.b, now.tile * kTile + lane) : -1;
+#pragma unroll 1
+    for (int half = 0; half < kTile / PAGES; ++half) {
+      Elems hi[PAGES], lo[PAGES];
 #pragma unroll
       for (int j = 0; j < PAGES; ++j) {
-        s[j] = s[PAGES + j] = 0.f;
+        const int at = __shfl_sync(0xffffffffu, of_tile, half * PAGES + j);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float k = x.x[e] >= 0.f ? hi[j].x[e] : lo[j].x[e];
-          s[j] = fmaf(x.x[e], k, s[j]);
-          s[PAGES + j] = fmaf(fabsf(x.x[e]), fabsf(k), s[PAGES + j]);
+        for (int e = 0; e < E; ++e) hi[j].x[e] = lo[j].x[e] = 0.f;
+        if (at >= 0) {
+          hi[j] = src_hi[(size_t)at * p.Hk * 32];
+          lo[j] = src_lo[(size_t)at * p.Hk * 32];
         }
       }
-      halve_sums(s, lane);
-      nan |= s[0] != s[0];
-      best = fmaxf(best, s[0]);
-      far = s[0] == s[0] ? fmaxf(far, s[0]) : INFINITY;
-    }
-    const int page = page0 + lane / 2 % PAGES, at = __shfl_sync(0xffffffffu, mine, lane / 2 % PAGES);
-    if (lane >= 16) {
-      if (at >= 0) bound = fmaxf(bound, far);
-    } else if (page < N) {
-      const float s = at < 0 ? -INFINITY : nan ? NAN : best;
-      if (lane % 2 == 0) p.score[(size_t)unit * p.max_pages + page] = s;
-      if (page >= p.n_first && page < N - p.n_last) {
-        odd |= !(fabsf(s) < INFINITY);
-        least = fminf(least, s);
-        most = fmaxf(most, s);
+      float best = -INFINITY, far = 0.f;                                 // lanes 0 .. 15: score of page lane / 2; the others: S of page (lane - 16) / 2
+      bool nan = false;
+      for (int h = 0; h < p.G; ++h) {
+        const Elems x = *reinterpret_cast<const Elems*>(src_q + h * p.q_head);
+        float s[2 * PAGES];
+#pragma unroll
+        for (int j = 0; j < PAGES; ++j) {
+          s[j] = s[PAGES + j] = 0.f;
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const float k = x.x[e] >= 0.f ? hi[j].x[e] : lo[j].x[e];
+            s[j] = fmaf(x.x[e], k, s[j]);
+            s[PAGES + j] = fmaf(fabsf(x.x[e]), fabsf(k), s[PAGES + j]);
+          }
+        }
+        halve_sums(s, lane);
+        nan |= s[0] != s[0];
+        best = fmaxf(best, s[0]);
+        far = s[0] == s[0] ? fmaxf(far, s[0]) : INFINITY;
+      }
+      const int i = half * PAGES + lane / 2 % PAGES, page = now.tile * kTile + i, at = __shfl_sync(0xffffffffu, of_tile, i);
+      if (lane >= 16) {
+        if (at >= 0) bound = fmaxf(bound, far);
+      } else if (page < now.N) {
+        const float s = at < 0 ? -INFINITY : nan ? NAN : best;
+        if (lane % 2 == 0) p.score[(size_t)unit * p.max_pages + page] = s;
+        if (page >= p.n_first && page < now.N - p.n_last) {
+          odd |= !(fabsf(s) < INFINITY);
+          least = fminf(least, s);
+          most = fmaxf(most, s);
+        }
       }
     }
+    leave_tile(p.tile + (size_t)unit * p.tiles + now.tile, bound * error_factor<float>(), least, most, odd);
   }
-  leave_chunk<float>(p, unit, chunk, bound, least, most, odd);
 }
 
 // A page's score for one head in fp64, by eight lanes (all 32 of the warp call).  `at`: where the page lies, -1: nowhere.
@@ -401,9 +407,9 @@ __global__ void __launch_bounds__(SEL_THREADS, 1024 / SEL_THREADS) page_select_k
   const float* score = p.score + (size_t)unit * p.max_pages;
   for (int i = tid; i < min(p.max_pages, SEL_KEEP); i += SEL_THREADS)
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(kept + i)), "l"(score + i) : "memory");
-  const bool counts = tid / 32 * 32 < p.chunks;
+  const float4* of_tile = reinterpret_cast<const float4*>(p.tile + (size_t)unit * p.tiles);
   float4 known = make_float4(0.f, INFINITY, -INFINITY, 0.f);
-  if (tid < p.chunks) known = *reinterpret_cast<const float4*>(&p.chunk[(size_t)unit * p.chunks + tid]);
+  if (tid < p.tiles) known = of_tile[tid];
   const int N = pages_held(p, b), n = min(N, p.K);
   int32_t* sel = p.sel + (size_t)unit * p.K;
   if (kvh == 0 && tid == 0) p.n_sel[b] = n;
@@ -437,15 +443,27 @@ __global__ void __launch_bounds__(SEL_THREADS, 1024 / SEL_THREADS) page_select_k
   auto below = [](int pages, int word) { return pages >= word * 32 + 32 ? 0xffffffffu : pages <= word * 32 ? 0u : (1u << (pages - word * 32)) - 1; };
   for (int i = tid; i < words; i += SEL_THREADS) taken[i] = below(first, i) | (below(N, i) & ~below(last, i));    // the ones that are always taken
   __syncthreads();
-  if (counts) {
-    const int lw = __reduce_min_sync(0xffffffffu, ordered(known.y)), hw = __reduce_max_sync(0xffffffffu, ordered(known.z));
-    const int e = __reduce_max_sync(0xffffffffu, __float_as_int(known.x));     // (not negative, not a NaN)
-    const bool odd = __any_sync(0xffffffffu, __float_as_int(known.w) != 0);
-    if (lane == 0) {
-      atomicMin(&s_lo, lw);
-      atomicMax(&s_hi, hw);
-      atomicMax(&s_bound, e);
-      if (odd) s_odd = 1;
+  {
+    const int tiles = (N + kTile - 1) / kTile;
+    if (tid >= tiles) known = make_float4(0.f, INFINITY, -INFINITY, 0.f);
+    bool odd = __float_as_int(known.w) != 0;
+    for (int i = tid + SEL_THREADS; i < tiles; i += SEL_THREADS) {
+      const float4 k = of_tile[i];
+      known.x = fmaxf(known.x, k.x);
+      known.y = fminf(known.y, k.y);
+      known.z = fmaxf(known.z, k.z);
+      odd |= __float_as_int(k.w) != 0;
+    }
+    if (tid / 32 * 32 < tiles) {
+      const int lw = __reduce_min_sync(0xffffffffu, ordered(known.y)), hw = __reduce_max_sync(0xffffffffu, ordered(known.z));
+      const int e = __reduce_max_sync(0xffffffffu, __float_as_int(known.x));   // (not negative, not a NaN)
+      odd = __any_sync(0xffffffffu, odd);
+      if (lane == 0) {
+        atomicMin(&s_lo, lw);
+        atomicMax(&s_hi, hw);
+        atomicMax(&s_bound, e);
+        if (odd) s_odd = 1;
+      }
     }
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
@@ -586,18 +604,23 @@ __global__ void __launch_bounds__(SEL_THREADS, 1024 / SEL_THREADS) page_select_k
   }
 }
 
-int plan_select(int dtype, int B, int H, int Hk, int head_dim, int max_pages, size_t* score_bytes, size_t* bound_bytes, size_t* again_bytes, int max_len, int* chunks) {
+struct SelectPlan {
+  int ctas, tiles;
+  size_t score_bytes, tile_bytes, again_bytes;
+};
+int plan_select(int dtype, int B, int H, int Hk, int head_dim, int max_pages, int max_len, SelectPlan* g) {
   if (dtype != CERB_F32 && dtype != CERB_BF16) return CERB_E_ARG;
   if (B < 0 || H < 1 || Hk < 1 || H % Hk || (head_dim != 64 && head_dim != 128) || max_pages < 1 || max_pages > kMaxSelectPages) return CERB_E_SHAPE;
-  if (H / Hk > 64 || (long long)B * Hk > 0x7fffffll) return CERB_E_SHAPE;
+  if (H / Hk > 64 || Hk > 0xffff || (long long)B * Hk > 0x7fffffll) return CERB_E_SHAPE;
   const long long units = (long long)B * Hk;
-  // as many CTAs as run at once, of no less than a round of their warps
-  const int held = (int)(((long long)max_len + CERB_PAGE - 1) / CERB_PAGE), per = (dtype == CERB_BF16 ? 16 : 8) * SC_WARPS;
-  const long long most = (std::min(held, max_pages) + per - 1) / per, want = units ? 148 * (dtype == CERB_BF16 ? 3 : 4) / units : 1;
-  *chunks = (int)std::max(1ll, std::min({most, want, (long long)kMaxChunks}));
-  *score_bytes = ((size_t)units * max_pages * sizeof(float) + 255) & ~(size_t)255;
-  *bound_bytes = ((size_t)units * *chunks * sizeof(ChunkScores) + 255) & ~(size_t)255;
-  *again_bytes = (size_t)units * max_pages * sizeof(unsigned long long);
+  g->tiles = (max_pages + kTile - 1) / kTile;
+  // as many CTAs as run at once, of no less than a tile to a warp
+  const int held = (int)std::min(((long long)max_len + CERB_PAGE - 1) / CERB_PAGE, (long long)max_pages);
+  const long long most = (units * ((held + kTile - 1) / kTile) + SC_WARPS - 1) / SC_WARPS;
+  g->ctas = (int)std::max(1ll, std::min(most, 148ll * (dtype == CERB_BF16 ? 3 : 4)));
+  g->score_bytes = ((size_t)units * max_pages * sizeof(float) + 255) & ~(size_t)255;
+  g->tile_bytes = ((size_t)units * g->tiles * sizeof(TileScores) + 255) & ~(size_t)255;
+  g->again_bytes = (size_t)units * max_pages * sizeof(unsigned long long);
   return CERB_OK;
 }
 
@@ -620,10 +643,9 @@ extern "C" {
 int cerb_page_select_scratch_bytes(int32_t dtype, int32_t B, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_pages, int32_t max_len,
                                    size_t* bytes_out) {
   if (!bytes_out || max_len < 1) return CERB_E_ARG;
-  size_t s, e, g;
-  int chunks;
-  CERB_TRY(plan_select(dtype, B, n_heads, n_kv_heads, head_dim, max_pages, &s, &e, &g, max_len, &chunks));
-  *bytes_out = s + e + g;
+  SelectPlan g;
+  CERB_TRY(plan_select(dtype, B, n_heads, n_kv_heads, head_dim, max_pages, max_len, &g));
+  *bytes_out = g.score_bytes + g.tile_bytes + g.again_bytes;
   return CERB_OK;
 }
 
@@ -631,13 +653,13 @@ int cerb_page_select(const cerb_page_select_args* a, void* stream) {
   if (!a || (a->B > 0 && (!a->q || !a->k_min || !a->k_max || !a->page_table || !a->len || !a->sel || !a->n_sel))) return CERB_E_ARG;
   if (a->n_pool_pages < 1 || a->max_len < 1 || a->n_first < 0 || a->n_last < 0 || a->max_sel < 1) return CERB_E_ARG;
   if ((long long)a->n_first + a->n_last > a->max_sel) return CERB_E_SHAPE;
-  size_t s, e, g;
-  int chunks;
-  CERB_TRY(plan_select(a->dtype, a->B, a->n_heads, a->n_kv_heads, a->head_dim, a->max_pages, &s, &e, &g, a->max_len, &chunks));
+  SelectPlan g;
+  CERB_TRY(plan_select(a->dtype, a->B, a->n_heads, a->n_kv_heads, a->head_dim, a->max_pages, a->max_len, &g));
   const int es = a->dtype == CERB_BF16 ? 2 : 4;
   if (a->q_row_stride * es % 16 || a->q_head_stride * es % 16) return CERB_E_ARG;
   if (((uintptr_t)a->q | (uintptr_t)a->k_min | (uintptr_t)a->k_max | (uintptr_t)a->scratch) & 15) return CERB_E_ARG;
-  if (s + e + g > a->scratch_bytes || (s + e + g && !a->scratch)) return CERB_E_NOMEM;
+  const size_t need = g.score_bytes + g.tile_bytes + g.again_bytes;
+  if (need > a->scratch_bytes || (need && !a->scratch)) return CERB_E_NOMEM;
   if (a->B == 0) return CERB_OK;
   SelectParams p;
   memset(&p, 0, sizeof(p));
@@ -649,8 +671,8 @@ int cerb_page_select(const cerb_page_select_args* a, void* stream) {
   p.sel = a->sel;
   p.n_sel = a->n_sel;
   p.score = (float*)a->scratch;
-  p.chunk = (ChunkScores*)((char*)a->scratch + s);
-  p.again = (unsigned long long*)((char*)a->scratch + s + e);
+  p.tile = (TileScores*)((char*)a->scratch + g.score_bytes);
+  p.again = (unsigned long long*)((char*)a->scratch + g.score_bytes + g.tile_bytes);
   p.q_row = a->q_row_stride;
   p.q_head = a->q_head_stride;
   p.B = a->B;
@@ -662,13 +684,12 @@ int cerb_page_select(const cerb_page_select_args* a, void* stream) {
   p.K = a->max_sel;
   p.n_first = a->n_first;
   p.n_last = a->n_last;
-  p.chunks = chunks;
+  p.tiles = g.tiles;
   cudaStream_t st = (cudaStream_t)stream;
   const bool big = a->head_dim == 128, bf = a->dtype == CERB_BF16;
   const unsigned units = (unsigned)(a->B * a->n_kv_heads);
   auto score = bf ? (big ? page_score_bf16_kernel<128> : page_score_bf16_kernel<64>) : (big ? page_score_f32_kernel<128> : page_score_f32_kernel<64>);
-  const size_t q_smem = bf ? (size_t)(p.G + 7) / 8 * 8 * (a->head_dim + 8) * sizeof(bf16) : (size_t)p.G * a->head_dim * sizeof(float);
-  if (launch_pdl(score, dim3(units * (unsigned)chunks), dim3(SC_WARPS * 32), q_smem, st, p) != cudaSuccess) return CERB_E_CUDA;
+  if (launch_pdl(score, dim3((unsigned)g.ctas), dim3(SC_WARPS * 32), 0, st, p) != cudaSuccess) return CERB_E_CUDA;
   const size_t smem = ((size_t)a->max_pages + 31) / 32 * sizeof(unsigned) + std::min(a->max_pages, SEL_KEEP) * sizeof(float);
   // (twice the threads while every unit has an SM to itself)
   if (units <= 148)

@@ -69,66 +69,6 @@ __device__ __forceinline__ PageRef page_ref(const PagedParams& p, int first, int
   return r;
 }
 
-// ---- shares: the items of all sequences and heads one after another, cut into one share per CTA ----
-struct Share {
-  long long begin, end, size;   // items; of every CTA's share
-  int b;                        // the sequence that begin lies in,
-  long long off;                // and where in it
-};
-__device__ __forceinline__ Share share_of(const PagedParams& p) {
-  __shared__ long long s_sum[PA_WARPS], s_off;
-  __shared__ int s_b;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const bool few = p.B <= 32;                                            // every warp for itself
-  const int per = few ? 1 : (p.B + PA_WARPS * 32 - 1) / (PA_WARPS * 32);
-  const int b0 = min(p.B, (few ? lane : tid) * per), b1 = min(p.B, b0 + per);
-  const long long uh = (long long)p.Hk * p.units_h;
-  long long mine = 0;
-  for (int b = b0; b < b1; ++b) mine += span_of(p, b).items * uh;
-  long long sum = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long u = __shfl_up_sync(0xffffffffu, sum, o);
-    if (lane >= o) sum += u;
-  }
-  long long total = __shfl_sync(0xffffffffu, sum, 31);
-  if (!few) {
-    if (lane == 31) s_sum[warp] = sum;
-    __syncthreads();
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < PA_WARPS; ++w) {
-      if (w < warp) sum += s_sum[w];
-      total += s_sum[w];
-    }
-  }
-  Share s;
-  const long long even = total >> 32 ? (total + gridDim.x - 1) / gridDim.x : ((unsigned)total + (gridDim.x - 1)) / gridDim.x;
-  s.size = max(even, (long long)p.min_share);
-  s.begin = min(total, s.size * blockIdx.x);
-  s.end = min(total, s.begin + s.size);
-  const bool here = s.begin >= sum - mine && s.begin < sum;
-  long long at = sum - mine;
-  int b = b0;
-  if (here)
-    for (;; ++b) {
-      const long long n = span_of(p, b).items * uh;
-      if (s.begin < at + n) break;
-      at += n;
-    }
-  if (few) {
-    const int from = max(__ffs(__ballot_sync(0xffffffffu, here)) - 1, 0);
-    s.b = __shfl_sync(0xffffffffu, b, from);
-    s.off = s.begin - __shfl_sync(0xffffffffu, at, from);
-  } else {
-    if (here) { s_b = b; s_off = s.begin - at; }
-    __syncthreads();
-    s.b = s_b;
-    s.off = s_off;
-  }
-  return s;
-}
-
 // The running maxima, sums and unnormalised outputs of a CTA's warps.
 template <int DH, int HEADS>
 struct alignas(16) Sums {                                                // (written and sent in pieces of 8 bytes)
@@ -507,8 +447,8 @@ __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_
   __shared__ Sums<DH, HEADS> sums;
   griddep_wait();
   griddep_launch();
-  const Share sh = share_of(p);
   const long long uh = (long long)p.Hk * p.units_h;
+  const Share sh = share_of(p.B, [&](int b) { return span_of(p, b).items * uh; }, blockIdx.x, gridDim.x, p.min_share);
   // sequences without anything to look at
   for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
     if (span_of(p, b).items) continue;

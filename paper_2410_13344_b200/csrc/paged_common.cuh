@@ -34,4 +34,45 @@ __device__ __forceinline__ void halve_sums(float (&x)[N], int lane) {
   }
 }
 
+// The items of all sequences one after another (items(b) of sequence b), cut into equal shares.
+struct Share {
+  long long begin, end, size;   // items; of every share
+  int b;                        // the sequence that begin lies in,
+  long long off;                // and where in it
+};
+// Share `index` of `shares`, each of min_share items at least.  By a warp, which sums the items up for itself: a few hundred sequences
+// are a few loads to a lane, and no barrier.
+template <typename F>
+__device__ __forceinline__ Share share_of(int B, F items, int index, int shares, int min_share) {
+  const int lane = threadIdx.x & 31, per = (B + 31) / 32, b0 = min(B, lane * per), b1 = min(B, b0 + per);
+  long long mine = 0;
+#pragma unroll 4
+  for (int b = b0; b < b1; ++b) mine += items(b);
+  long long sum = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long u = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += u;
+  }
+  const long long total = __shfl_sync(0xffffffffu, sum, 31);
+  Share s;
+  const long long even = total >> 32 ? (total + shares - 1) / shares : ((unsigned)total + (unsigned)(shares - 1)) / (unsigned)shares;
+  s.size = max(even, (long long)min_share);
+  s.begin = min(total, s.size * index);
+  s.end = min(total, s.begin + s.size);
+  const bool here = s.begin >= sum - mine && s.begin < sum;
+  long long at = sum - mine;
+  int b = b0;
+  if (here)
+    for (;; ++b) {
+      const long long n = items(b);
+      if (s.begin < at + n) break;
+      at += n;
+    }
+  const int from = max(__ffs(__ballot_sync(0xffffffffu, here)) - 1, 0);
+  s.b = __shfl_sync(0xffffffffu, b, from);
+  s.off = s.begin - __shfl_sync(0xffffffffu, at, from);
+  return s;
+}
+
 }  // namespace cerb
