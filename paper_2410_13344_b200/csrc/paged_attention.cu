@@ -623,10 +623,13 @@ struct PagedPlan {
   int heads_unit, units_h, ctas, min_share, joins, together;
   long long units;
 };
-#ifndef MINSHARE
-#define MINSHARE 8
-#define TOGETHER_ITEMS 8
-#endif
+// A cluster per unit, as many CTAs as make the grid one wave and find a page for each of their warps, while the longest sequence leaves a warp no more than 12 pages;
+// shares and a join beyond that.  (bf16, 4 x 8 heads of 128, all sequences alike / between half as long and as long, every fourth idle; us with
+// clusters, with shares: 64 units of 8 pages 5.8 / 5.8, 7.0 / 13.0; 8 of 400 11.4 / 9.6, 13.4 / 15.2; 192 of 64 19.7 / 17.9, 23.3 / 19.5; 1 of 400 8.4, 9.8.  More than
+// that to a warp, the longest decide: 256 units of 64 29.6 / 27.9, 28.2 / 21.8; 128 of 160 35.8 / 32.2, 36.4 / 24.3; 1 of 1000 14.1, 10.6.)
+constexpr int kClusterPages = 12;
+// Shares of fewer items cost more in joins than they save.  (1 unit of 64 pages, 4 / 8 / 16 items: 7.6 / 7.8 / 9.2 us; 64 of 24: 10.9 / 10.2 / 11.6.)
+constexpr int kMinShare = 8;
 // max_items: pages that a sequence can have to be looked at (a window may begin and end inside one)
 int plan_paged(int dtype, int B, int H, int Hk, int head_dim, int max_len, int window, int max_sel, PagedPlan* g) {
   if (dtype != CERB_F32 && dtype != CERB_BF16) return CERB_E_ARG;
@@ -641,13 +644,10 @@ int plan_paged(int dtype, int B, int H, int Hk, int head_dim, int max_len, int w
   if (g->units * std::max(g->heads_unit, PA_CLUSTER) > 0x7fffffffll) return CERB_E_SHAPE;
   const int at_once = 148 * (bf ? (g->heads_unit == 8 ? ctas_per_sm<bf16, 8>() : ctas_per_sm<bf16, 16>())
                                 : g->heads_unit == 8 ? ctas_per_sm<float, 8>() : g->heads_unit == 4 ? ctas_per_sm<float, 4>() : ctas_per_sm<float, 2>());
-  g->together = 0;
-  if (g->units * items <= (long long)at_once * PA_WARPS * TOGETHER_ITEMS) {
-    g->together = 1;
-    while (g->together < PA_CLUSTER && g->units * g->together * 2 <= at_once && g->together * 2 * PA_WARPS <= items + PA_WARPS) g->together *= 2;
-    if (items > (long long)g->together * PA_WARPS * 4 * TOGETHER_ITEMS) g->together = 0;
-  }
-  g->min_share = MINSHARE;
+  g->together = 1;
+  while (g->together < PA_CLUSTER && g->units * g->together * 2 <= at_once && g->together * 2 * PA_WARPS <= items + PA_WARPS) g->together *= 2;
+  if (items > g->together * PA_WARPS * kClusterPages) g->together = 0;
+  g->min_share = kMinShare;
   if (g->together) {
     g->ctas = (int)g->units * g->together;
     g->joins = 0;
