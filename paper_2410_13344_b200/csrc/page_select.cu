@@ -41,6 +41,7 @@ struct SelectParams {
   unsigned long long* again;   // [unit][max_pages]: scores of 64 bits as ordered whole numbers
   long long q_row, q_head;     // elements
   int B, H, Hk, G, max_pages, n_pool_pages, K, n_first, n_last, tiles;
+  int scored;                  // 0: no scores have been computed, since no sequence was to be longer than max_sel pages
 };
 
 __device__ __forceinline__ int pages_held(const SelectParams& p, int b) {
@@ -405,11 +406,11 @@ __global__ void __launch_bounds__(SEL_THREADS, 1024 / SEL_THREADS) page_select_k
   griddep_launch();
   // what does not need the length is on its way before it: the scores (of the whole table's row, whatever lies behind the last) and what is known of them
   const float* score = p.score + (size_t)unit * p.max_pages;
-  for (int i = tid; i < min(p.max_pages, SEL_KEEP); i += SEL_THREADS)
+  for (int i = tid; p.scored && i < min(p.max_pages, SEL_KEEP); i += SEL_THREADS)
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(kept + i)), "l"(score + i) : "memory");
   const float4* of_tile = reinterpret_cast<const float4*>(p.tile + (size_t)unit * p.tiles);
   float4 known = make_float4(0.f, INFINITY, -INFINITY, 0.f);
-  if (tid < p.tiles) known = of_tile[tid];
+  if (p.scored && tid < p.tiles) known = of_tile[tid];
   const int N = pages_held(p, b), n = min(N, p.K);
   int32_t* sel = p.sel + (size_t)unit * p.K;
   if (kvh == 0 && tid == 0) p.n_sel[b] = n;
@@ -421,7 +422,7 @@ __global__ void __launch_bounds__(SEL_THREADS, 1024 / SEL_THREADS) page_select_k
   }
   const int first = p.n_first, last = N - p.n_last;                      // pages first .. last - 1 are up for selection
   const int want = p.K - first - p.n_last;                               // (K >= n_first + n_last, and N > K)
-  const bool keep = N <= SEL_KEEP;
+  const bool keep = N <= SEL_KEEP;                                       // (without scores: whatever lies there, which nothing is decided by)
   // f(page, score) for this thread's pages
   auto each = [&](auto f) {
     if (keep) {
@@ -443,7 +444,7 @@ __global__ void __launch_bounds__(SEL_THREADS, 1024 / SEL_THREADS) page_select_k
   auto below = [](int pages, int word) { return pages >= word * 32 + 32 ? 0xffffffffu : pages <= word * 32 ? 0u : (1u << (pages - word * 32)) - 1; };
   for (int i = tid; i < words; i += SEL_THREADS) taken[i] = below(first, i) | (below(N, i) & ~below(last, i));    // the ones that are always taken
   __syncthreads();
-  {
+  if (p.scored) {
     const int tiles = (N + kTile - 1) / kTile;
     if (tid >= tiles) known = make_float4(0.f, INFINITY, -INFINITY, 0.f);
     bool odd = __float_as_int(known.w) != 0;
@@ -470,7 +471,7 @@ __global__ void __launch_bounds__(SEL_THREADS, 1024 / SEL_THREADS) page_select_k
   __syncthreads();
   const float E = __int_as_float(s_bound);
   float lo = from_ordered(s_lo), hi = from_ordered(s_hi);
-  const bool all_again = s_odd || !(E < INFINITY);                       // scores that are not finite decide nothing
+  const bool all_again = !p.scored || s_odd || !(E < INFINITY);          // scores that are not finite decide nothing
   int above = 0;                                                         // pages above hi
   float t_lo = -INFINITY, t_hi = INFINITY;
   if (!all_again && want > 0) {
@@ -689,7 +690,9 @@ int cerb_page_select(const cerb_page_select_args* a, void* stream) {
   const bool big = a->head_dim == 128, bf = a->dtype == CERB_BF16;
   const unsigned units = (unsigned)(a->B * a->n_kv_heads);
   auto score = bf ? (big ? page_score_bf16_kernel<128> : page_score_bf16_kernel<64>) : (big ? page_score_f32_kernel<128> : page_score_f32_kernel<64>);
-  if (launch_pdl(score, dim3((unsigned)g.ctas), dim3(SC_WARPS * 32), 0, st, p) != cudaSuccess) return CERB_E_CUDA;
+  // (a sequence that is longer than the caller said has all of its pages scored in fp64)
+  p.scored = ((long long)a->max_len + CERB_PAGE - 1) / CERB_PAGE > a->max_sel;
+  if (p.scored && launch_pdl(score, dim3((unsigned)g.ctas), dim3(SC_WARPS * 32), 0, st, p) != cudaSuccess) return CERB_E_CUDA;
   const size_t smem = ((size_t)a->max_pages + 31) / 32 * sizeof(unsigned) + std::min(a->max_pages, SEL_KEEP) * sizeof(float);
   // (twice the threads while every unit has an SM to itself)
   if (units <= 148)

@@ -375,6 +375,16 @@ def test_selection_of_very_long_caches(N, K):
     assert sel[0, 0].tolist() == want.tolist() and n_sel.tolist() == [K]
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("hint", [1, 100, 16 * 30, 16 * 30 + 1, 60000])
+def test_selection_from_caches_longer_than_was_said(dtype, hint):
+    lens = [16 * 30, 16 * 30 + 1, 9000, 0, 12345]
+    c = Cache(lens, 2, 64, dtype, 5)
+    q, gq = c.queries(6, 5)
+    sel, n_sel = binding.page_select(gq, c.k_min.cuda(), c.k_max.cuda(), c.gpu[2], c.glens, 30, hint)
+    check_lists(sel, n_sel, ref.select(q, c.k_min, c.k_max, c.table, lens, 30), 30)
+
+
 def test_selection_with_queries_that_are_not_finite_and_pages_outside_the_pool():
     lo, hi = score_cache("plain", "bf16", 500)
     table = torch.arange(500, dtype=torch.int32)[None].repeat(2, 1)
