@@ -19,7 +19,7 @@ namespace cerb {
 namespace {
 
 constexpr int PA_WARPS = 4;
-constexpr int PA_CLUSTER = 16;        // CTAs of a cluster at most (more than eight: where the device lets them)
+constexpr int PA_CLUSTER = 16;        // CTAs of a cluster at most
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct PagedParams {

@@ -98,8 +98,8 @@ void* operand(const at::Tensor& t, int64_t rows, int64_t heads, int64_t dh, cons
               const char* why) {
   if (t.dim() != 3 || t.size(0) != rows || t.size(1) != heads || t.size(2) != dh || t.scalar_type() != like.scalar_type() || t.stride(2) != 1) refuse(what, why);
   if (!t.is_cuda() || t.get_device() != device) refuse(what, "tensors are on different devices");
-  *row = t.stride(0);
-  *head = t.stride(1);
+  *row = rows > 1 ? t.stride(0) : 0;               // (torch leaves any stride where there is nothing to step over)
+  *head = heads > 1 ? t.stride(1) : 0;
   return t.data_ptr();
 }
 

@@ -1,4 +1,7 @@
 // Bookkeeping of a paged KV cache, and the append into it.
+//
+// Tree attention reads lengths, page tables and committed keys ahead of its wait for the kernel in front.  So the kernels here, which write them, do not
+// let the next kernel start before they are complete.
 #include <string.h>
 
 #include <algorithm>
@@ -78,7 +81,6 @@ __global__ void __launch_bounds__(THREADS, 1) pages_plan_kernel(const PagesParam
   const unsigned cta = ALONE ? 0 : blockIdx.x, ctas = ALONE ? 1 : gridDim.x;
   if (tid == 0) s_taken = 0;
   griddep_wait();
-  griddep_launch();
   const int n_free = min(max(*p.n_free, 0), p.free_cap);
   long long rows_before = 0;
   int pages_before = 0;
@@ -160,7 +162,6 @@ __global__ void __launch_bounds__(THREADS, 1) pages_plan_kernel(const PagesParam
 __global__ void __launch_bounds__(PLAN_THREADS, 1) pages_grant_kernel(const PagesParams p) {
   __shared__ int red_pages[32];
   griddep_wait();
-  griddep_launch();
   int taken = 0;
   for (int b = threadIdx.x; b < p.B; b += PLAN_THREADS) {
     const int n = p.granted[b], len = held_tokens(p, b);
@@ -181,7 +182,6 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) pages_trim_kernel(const Pages
   const int tid = threadIdx.x;
   const unsigned cta = blockIdx.x;
   griddep_wait();
-  griddep_launch();
   const int n_free = min(max(*p.n_free, 0), p.free_cap);
   int total = 0;
   for (int b0 = 0; b0 < p.B; b0 += PLAN_THREADS) {
@@ -273,7 +273,6 @@ __global__ void __launch_bounds__(256, 4) kv_append_kernel(const AppendParams p)
   const bool sums = !values && p.k_min != nullptr;
   const unsigned group = LANES == 32 ? 0xffffffffu : ((1u << LANES) - 1) << ((threadIdx.x & 31) / LANES * LANES);
   griddep_wait();
-  griddep_launch();
   auto page_of = [&](long long t) {
     const int s = t >= 0 && t < p.T ? p.slot[t] : -1;
     return s >= 0 && s < p.n_slots ? s / CERB_PAGE : -1;

@@ -518,6 +518,63 @@ def test_a_captured_step_replays_as_the_requests_grow():
     assert s.state[0].tolist() == [n + 21 for n in prompt]
 
 
+def test_tree_attention_right_behind_an_append_and_a_plan():
+    """The library's tree attention reads lengths, tables and committed keys ahead of its wait for the kernel in front: behind the calls that change them
+    it must find them changed."""
+    B, H, D, mp = 4, 8, 128, 40
+    g = torch.Generator(device="cuda").manual_seed(4)
+
+    def normal(*size):
+        return torch.empty(*size, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+
+    k_pool, v_pool = normal(B * mp, H, PAGE, D), normal(B * mp, H, PAGE, D)
+    one = torch.tensor([[1, 0, 0]], dtype=torch.int64, device="cuda")
+    for step in range(12):
+        state = [torch.zeros(B, dtype=torch.int32, device="cuda"), torch.zeros(B, mp, dtype=torch.int32, device="cuda"),
+                 torch.randperm(B * mp, device="cuda", generator=g).to(torch.int32), i32([B * mp])]
+        lens = [37 + 50 * b + step for b in range(B)]
+        rows = sum(lens)
+        k, v, q = normal(rows, H, D), normal(rows, H, D), normal(B, 1, H, D)
+        n_new, less = i32(lens), i32([n - 1 for n in lens])
+        _, _, scratch = binding.tree_attention(q, k_pool, v_pool, state[1], state[0], one, 0.1, max(lens))
+        torch.cuda.synchronize()
+        p = binding.pages_plan(n_new, *state, rows)
+        # a tree of one node sits behind the committed keys: the last token's key is its own
+        binding.kv_append(k, v, p.slot, k_pool, v_pool)
+        late, _, _ = binding.tree_attention(q, k_pool, v_pool, state[1], less, one, 0.1, max(lens), scratch=scratch)
+        state[0].copy_(less)
+        keep = less.clone()
+        torch.cuda.synchronize()
+        binding.pages_plan(i32([0] * B), *state, 0)
+        again, _, _ = binding.tree_attention(q, k_pool, v_pool, state[1], keep, one, 0.1, max(lens), scratch=scratch)
+        own, _ = binding.paged_attention(q[:, 0], k_pool, v_pool, state[1], n_new, 0.1, max(lens))
+        assert torch.equal(late, again), step
+        assert float((late[:, 0].float() - own.float()).abs().max()) < 0.03, step      # (two kernels: each within 2^-8 of its weights and its result, values of 3 to 4)
+
+
+def test_operands_with_strides_of_their_own():
+    c = Cache([300], 1, 64, "bf16", 71)
+    q, gq = c.queries(8, 6)
+    want = ref.attention(q[:, ::2], c.k_pool, c.v_pool, c.table, [300], 0.1)
+    check(*binding.paged_attention(gq[:, ::2], *c.gpu, c.glens, 0.1, 300), want)
+    # dimensions of one: any stride will do
+    odd = torch.empty(5000, dtype=torch.bfloat16, device="cuda")
+    one = odd[:64].copy_(gq[0, 3]).as_strided((1, 1, 64), (3, 7, 1))
+    check(*binding.paged_attention(one, *c.gpu, c.glens, 0.1, 300), ref.attention(q[:, 3:4], c.k_pool, c.v_pool, c.table, [300], 0.1))
+    pool = [torch.zeros(2, 1, PAGE, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    binding.kv_append(one, one, i32([17]), *pool)
+    assert torch.equal(pool[0][1, 0, 1], gq[0, 3]) and int((pool[1] != 0).sum()) == int((gq[0, 3] != 0).sum())
+    # the same key for every row of a call
+    row = gq[0, 2:3][None].expand(5, 1, 64)
+    binding.kv_append(row, row, i32([0, 1, 2, -1, 4]), *pool)
+    assert torch.equal(pool[0][0, 0, :5], torch.stack([gq[0, 2]] * 3 + [torch.zeros_like(gq[0, 2]), gq[0, 2]]))
+    # not on 16 bytes
+    for bad in (odd[1:65].view(1, 1, 64), odd[:2 * 68].view(2, 1, 68)[:, :, :64]):
+        with pytest.raises(binding.CerbError) as e:
+            binding.kv_append(bad, bad, i32([0] * bad.shape[0]), *pool)
+        assert e.value.code == binding.E_ARG
+
+
 def test_calls_on_another_stream():
     c = Cache([3000, 70, 0], 2, 64, "bf16", 51)
     _, gq = c.queries(8, 6)

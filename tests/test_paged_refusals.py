@@ -179,3 +179,12 @@ def test_binding_wants_tensors_of_a_gpu():
         with pytest.raises(binding.CerbError) as e:
             call()
         assert e.value.code == binding.E_ARG
+
+
+def test_kernels_that_change_the_cache_release_nothing_early():
+    """Tree attention reads lengths, tables and committed keys ahead of its wait for the kernel in front: what writes them may not let it start early."""
+    import os
+    import re
+    text = open(os.path.join(os.path.dirname(binding.__file__), "csrc", "pages.cu")).read()
+    text = re.sub(r"//[^\n]*", "", text)
+    assert text.count("__global__") == text.count("griddep_wait()") == 4 and "griddep_launch" not in text
