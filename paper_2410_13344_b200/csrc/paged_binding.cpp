@@ -106,6 +106,13 @@ void* operand(const at::Tensor& t, int64_t rows, int64_t heads, int64_t dh, cons
 at::Tensor make(at::IntArrayRef sizes, at::ScalarType type, int device) {
   return at::empty(sizes, at::TensorOptions().dtype(type).device(at::kCUDA, (c10::DeviceIndex)device));
 }
+// `n` elements of a tensor's memory, as a tensor of their own.
+at::Tensor part(const at::Tensor& t, int64_t at, int64_t n) {
+  auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(t.storage()), t.key_set(), t.dtype());
+  impl->set_storage_offset(at);
+  impl->set_sizes_contiguous({n});
+  return at::Tensor(std::move(impl));
+}
 void* stream_of(int device) { return (void*)c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream(); }
 
 // Runs a call with the tensors' device current, and turns what is thrown into a Python error.
@@ -156,10 +163,17 @@ PyObject* pages_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {       // n_n
     if (rows < 0) refuse(what, "rows is negative");
     if (s.B > 8192 || rows > 1 << 30) refuse(what, "more than 8192 requests or 2^30 rows", CERB_E_SHAPE);        // (ahead of the allocations)
     const c10::cuda::OptionalCUDAGuard on(c10::Device(c10::kCUDA, (c10::DeviceIndex)device));
-    at::Tensor out[5] = {make({rows}, at::kInt, device), make({rows}, at::kInt, device), make({rows}, at::kInt, device), make({s.B + 1}, at::kInt, device),
-                         make({s.B}, at::kInt, device)};
+    // one piece of memory, each part on 16 bytes
+    const int64_t sizes[5] = {rows, rows, rows, s.B + 1, s.B};
+    int64_t at[6] = {0};
+    for (int i = 0; i < 5; ++i) at[i + 1] = at[i] + (sizes[i] + 3) / 4 * 4;
+    const at::Tensor all = make({at[5]}, at::kInt, device);
+    at::Tensor out[5];
     int32_t* p[5];
-    for (int i = 0; i < 5; ++i) p[i] = (int32_t*)out[i].data_ptr();
+    for (int i = 0; i < 5; ++i) {
+      out[i] = part(all, at[i], sizes[i]);
+      p[i] = (int32_t*)all.data_ptr() + at[i];
+    }
     done(lib.pages_plan(&s, want, rows, p[0], p[1], p[2], p[3], p[4], stream_of(device)), what);
     return PyObject_CallFunction(plan_class, "NNNNN", THPVariable_Wrap(out[0]), THPVariable_Wrap(out[1]), THPVariable_Wrap(out[2]), THPVariable_Wrap(out[3]),
                                  THPVariable_Wrap(out[4]));
