@@ -559,6 +559,36 @@ __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_
   }
 }
 
+// Every unit a warp, for many short sequences: nothing to meet, no barrier.
+template <typename T, int DH, int HEADS>
+__global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_attn_warp_kernel(const PagedParams p) {
+  __shared__ Sums<DH, HEADS> sums;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long unit = (long long)blockIdx.x * PA_WARPS + warp;
+  griddep_wait();
+  griddep_launch();
+  const int part = (int)(unit % p.units_h);
+  Piece c;
+  c.kvh = (int)(unit / p.units_h % p.Hk);
+  const long long b = unit / p.units_h / p.Hk;
+  if (b >= p.B) return;
+  c.b = (int)b;
+  c.head0 = c.kvh * p.G + part * HEADS;
+  c.heads = min(HEADS, p.G - part * HEADS);
+  c.item0 = -warp;                                                       // (all of the items are this warp's)
+  c.stride = 1;
+  if (p.window == 0 || p.sel) c.ahead = page_ref(p, 0, c.b, c.kvh, lane);
+  c.sp = span_of(p, c.b);
+  if (p.window > 0 && !p.sel) c.ahead = page_ref(p, c.sp.first, c.b, c.kvh, lane);
+  c.item1 = c.sp.items;
+  attend<T, DH, HEADS>(p, c, sums);
+  __syncwarp();
+  for (int i = lane; i < c.heads * DH; i += 32) {
+    const int h = i / DH, d = i % DH;
+    store_out<T>(p, (size_t)c.b * p.H + c.head0 + h, d, DH, sums.o[warp][h][d], sums.m[warp][h], sums.l[warp][h]);
+  }
+}
+
 // The parts of a unit as one.  A warp takes a head (heads_y of them per CTA) and every groups-th part.
 template <typename T, int DH>
 __global__ void __launch_bounds__(1024) paged_join_kernel(const PagedParams p, int heads_unit, int heads_y) {
@@ -620,7 +650,7 @@ __global__ void __launch_bounds__(1024) paged_join_kernel(const PagedParams p, i
 
 // How a call is cut up: heads of a unit, units of a KV head, CTAs (and of them in a cluster, 0: shares and a join).
 struct PagedPlan {
-  int heads_unit, units_h, ctas, min_share, joins, together;
+  int heads_unit, units_h, ctas, min_share, joins, together;          // together: -1 a warp per unit
   long long units;
 };
 // A cluster per unit, as many CTAs as make the grid one wave and find a page for each of their warps, while the longest sequence leaves a warp no more than 12 pages;
@@ -628,6 +658,10 @@ struct PagedPlan {
 // clusters, with shares: 64 units of 8 pages 5.8 / 5.8, 7.0 / 13.0; 8 of 400 11.4 / 9.6, 13.4 / 15.2; 192 of 64 19.7 / 17.9, 23.3 / 19.5; 1 of 400 8.4, 9.8.  More than
 // that to a warp, the longest decide: 256 units of 64 29.6 / 27.9, 28.2 / 21.8; 128 of 160 35.8 / 32.2, 36.4 / 24.3; 1 of 1000 14.1, 10.6.)
 constexpr int kClusterPages = 12;
+// Many short sequences: a warp per unit, while that is no more pages than these (four times as many where the units are more than one wave of CTAs).  (Pages of a sequence, all
+// alike, us with a CTA / a warp per unit: 384 units of 1 / 4 / 8 pages 6.6 / 7.7 / 9.0, 4.8 / 7.1 / 9.6; 1024 of 1 / 8 / 16 18.7 / 27.0 / 36.5, 6.8 / 17.3 / 28.8; 5120 of 1 / 8
+// 75 / 108, 19 / 59.)
+constexpr int kWarpPages = 4;
 // Shares of fewer items cost more in joins than they save.  (1 unit of 64 pages, 4 / 8 / 16 items: 7.6 / 7.8 / 9.2 us; 64 of 24: 10.9 / 10.2 / 11.6.)
 constexpr int kMinShare = 8;
 // max_items: pages that a sequence can have to be looked at (a window may begin and end inside one)
@@ -648,6 +682,12 @@ int plan_paged(int dtype, int B, int H, int Hk, int head_dim, int max_len, int w
   while (g->together < PA_CLUSTER && g->units * g->together * 2 <= at_once && g->together * 2 * PA_WARPS <= items + PA_WARPS) g->together *= 2;
   if (items > g->together * PA_WARPS * kClusterPages) g->together = 0;
   g->min_share = kMinShare;
+  if (g->units > at_once ? items <= 4 * kWarpPages : g->units * 2 > at_once && items <= kWarpPages) g->together = -1;
+  if (g->together < 0) {
+    g->ctas = (int)((g->units + PA_WARPS - 1) / PA_WARPS);
+    g->joins = 0;
+    return CERB_OK;
+  }
   if (g->together) {
     g->ctas = (int)g->units * g->together;
     g->joins = 0;
@@ -671,6 +711,7 @@ cudaError_t launch(const PagedPlan& g, const PagedParams& p, cudaStream_t st) {
     static std::atomic<uint64_t> done{0};
     if (allow_wide_clusters(paged_attn_cluster_kernel<T, DH, HEADS>, done) != CERB_OK) return cudaErrorInvalidValue;
   }
+  if (g.together < 0) return launch_pdl(paged_attn_warp_kernel<T, DH, HEADS>, dim3((unsigned)g.ctas), block, 0, st, p);
   if (g.together) return launch_pdl_cluster(paged_attn_cluster_kernel<T, DH, HEADS>, dim3((unsigned)g.ctas), block, 0, st, (unsigned)g.together, p);
   const cudaError_t rc = launch_pdl(paged_attn_kernel<T, DH, HEADS>, dim3((unsigned)g.ctas), block, 0, st, p);
   if (rc != cudaSuccess || g.ctas == 1) return rc;

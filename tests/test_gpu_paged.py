@@ -243,6 +243,24 @@ def test_attention_of_long_caches_in_splits(dtype, lens, window, hint):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("B,Hk,G,D,longest,window", [(120, 5, 1, 64, 60, 0), (120, 5, 1, 128, 200, 50), (75, 4, 3, 128, 64, 0), (90, 8, 9, 64, 250, 0), (60, 16, 2, 64, 33, 1),
+                                                     (300, 2, 17, 128, 40, 0)])
+def test_attention_of_many_short_sequences(dtype, B, Hk, G, D, longest, window):
+    rng = random.Random(B)
+    lens = [rng.choice([0, 1, 16, 17, longest, rng.randint(0, longest)]) for _ in range(B)]
+    lens[-1] = 0
+    c = Cache(lens, Hk, D, dtype, B)
+    q, gq = c.queries(Hk * G, 5)
+    want = ref.attention(q, c.k_pool, c.v_pool, c.table, lens, 0.2, window)
+    check(*binding.paged_attention(gq, *c.gpu, c.glens, 0.2, longest, window=window), want)
+    if not window:
+        # (and with lists: of all pages, which is the same, in another order)
+        pages = [ref.pages_of(n) for n in lens]
+        lists = [[list(range(n))[::-1] + [-1] * (max(pages) - n) for _ in range(Hk)] for n in pages]
+        check(*binding.paged_attention(gq, *c.gpu, c.glens, 0.2, longest, sel=i32(lists), n_sel=i32(pages)), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("size,scale", [(0.0, 1.0), (30.0, 1.0), (4.0, -0.3), (2.0, 0.0)])
 def test_attention_with_flat_peaked_and_negative_scores(dtype, size, scale):
     lens = [1, 50, 700]
