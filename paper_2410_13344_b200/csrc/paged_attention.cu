@@ -656,7 +656,8 @@ struct PagedPlan {
 // A cluster per unit, as many CTAs as make the grid one wave and find a page for each of their warps, while the longest sequence leaves a warp no more than 12 pages;
 // shares and a join beyond that.  (bf16, 4 x 8 heads of 128, all sequences alike / between half as long and as long, every fourth idle; us with
 // clusters, with shares: 64 units of 8 pages 5.8 / 5.8, 7.0 / 13.0; 8 of 400 11.4 / 9.6, 13.4 / 15.2; 192 of 64 19.7 / 17.9, 23.3 / 19.5; 1 of 400 8.4, 9.8.  More than
-// that to a warp, the longest decide: 256 units of 64 29.6 / 27.9, 28.2 / 21.8; 128 of 160 35.8 / 32.2, 36.4 / 24.3; 1 of 1000 14.1, 10.6.)
+// that to a warp, the longest decide: 256 units of 64 29.6 / 27.9, 28.2 / 21.8; 128 of 160 35.8 / 32.2, 36.4 / 24.3; 1 of 1000 14.1, 10.6.  And of more than one wave: 512 units
+// of 32 35.9 / 22.8, 30.3 / 23.8; 2048 of 24 82 / 56, 73 / 52.  fp32 from four heads of a unit on: half as many, 32 units of 300 pages 37 / 31, 34 / 23.)
 constexpr int kClusterPages = 12;
 // Many short sequences: a warp per unit, while that is no more pages than these (four times as many where the units are more than one wave of CTAs).  (Pages of a sequence, all
 // alike, us with a CTA / a warp per unit: 384 units of 1 / 4 / 8 pages 6.6 / 7.7 / 9.0, 4.8 / 7.1 / 9.6; 1024 of 1 / 8 / 16 18.7 / 27.0 / 36.5, 6.8 / 17.3 / 28.8; 5120 of 1 / 8
@@ -680,7 +681,7 @@ int plan_paged(int dtype, int B, int H, int Hk, int head_dim, int max_len, int w
                                 : g->heads_unit == 8 ? ctas_per_sm<float, 8>() : g->heads_unit == 4 ? ctas_per_sm<float, 4>() : ctas_per_sm<float, 2>());
   g->together = 1;
   while (g->together < PA_CLUSTER && g->units * g->together * 2 <= at_once && g->together * 2 * PA_WARPS <= items + PA_WARPS) g->together *= 2;
-  if (items > g->together * PA_WARPS * kClusterPages) g->together = 0;
+  if (g->units > at_once || items > (long long)g->together * PA_WARPS * (bf || g->heads_unit <= 2 ? kClusterPages : kClusterPages / 2)) g->together = 0;
   g->min_share = kMinShare;
   if (g->units > at_once ? items <= 4 * kWarpPages : g->units * 2 > at_once && items <= kWarpPages) g->together = -1;
   if (g->together < 0) {
