@@ -22,6 +22,9 @@ namespace {
 constexpr int SC_WARPS = 4;
 constexpr int SEL_KEEP = 8192;              // scores that shared memory keeps: those of caches of up to so many pages
 constexpr int SEL_LIST = 512;               // pages near the border that are ranked one against another
+// (Page, head) pairs of a unit up to which the selection scores all of its pages itself, in fp64, and no scores are computed ahead of it.  (us with / without, 4 heads, 8 units
+// and 256: 32 pages 7.9 / 6.2, 64 pages 7.9 / 9.4; one head: 64 pages 8.4 / 5.7, 128 7.7 / 9.0; 256 units of 8 heads: 16 pages 10.4 / 8.6, 32 pages 10.9 / 14.2.)
+constexpr int kScoreAlone = 128;
 constexpr int kMaxSelectPages = 1 << 17;    // (a bit mask of them lies in shared memory)
 
 // What is known of the scores of a tile of pages (of those of it that are up for selection).
@@ -41,7 +44,7 @@ struct SelectParams {
   unsigned long long* again;   // [unit][max_pages]: scores of 64 bits as ordered whole numbers
   long long q_row, q_head;     // elements
   int B, H, Hk, G, max_pages, n_pool_pages, K, n_first, n_last, tiles;
-  int scored;                  // 0: no scores have been computed, since no sequence was to be longer than max_sel pages
+  int scored;                  // 0: no scores have been computed, the sequences were to be too short for it
 };
 
 __device__ __forceinline__ int pages_held(const SelectParams& p, int b) {
@@ -691,7 +694,8 @@ int cerb_page_select(const cerb_page_select_args* a, void* stream) {
   const unsigned units = (unsigned)(a->B * a->n_kv_heads);
   auto score = bf ? (big ? page_score_bf16_kernel<128> : page_score_bf16_kernel<64>) : (big ? page_score_f32_kernel<128> : page_score_f32_kernel<64>);
   // (a sequence that is longer than the caller said has all of its pages scored in fp64)
-  p.scored = ((long long)a->max_len + CERB_PAGE - 1) / CERB_PAGE > a->max_sel;
+  const long long held = ((long long)a->max_len + CERB_PAGE - 1) / CERB_PAGE;
+  p.scored = held > a->max_sel && held * p.G > kScoreAlone;
   if (p.scored && launch_pdl(score, dim3((unsigned)g.ctas), dim3(SC_WARPS * 32), 0, st, p) != cudaSuccess) return CERB_E_CUDA;
   const size_t smem = ((size_t)a->max_pages + 31) / 32 * sizeof(unsigned) + std::min(a->max_pages, SEL_KEEP) * sizeof(float);
   // (twice the threads while every unit has an SM to itself)
