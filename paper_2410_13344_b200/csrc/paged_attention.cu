@@ -663,6 +663,9 @@ constexpr int kClusterPages = 12;
 // alike, us with a CTA / a warp per unit: 384 units of 1 / 4 / 8 pages 6.6 / 7.7 / 9.0, 4.8 / 7.1 / 9.6; 1024 of 1 / 8 / 16 18.7 / 27.0 / 36.5, 6.8 / 17.3 / 28.8; 5120 of 1 / 8
 // 75 / 108, 19 / 59.)
 constexpr int kWarpPages = 4;
+// Groups of more than eight heads in bf16: sixteen to a unit, which reads keys and values once for them; eight, and more CTAs, while those are no more pages than these in all.  (Heads of
+// 128, us with 16 / 8: 2 units of 256 pages 8.5 / 7.0, 32 of 64 14.0 / 8.4, 512 of 4 12.6 / 8.7; 32 of 256 19.9 / 17.0, ragged 11.9 / 15.6; 128 of 64 12.1 / 18.4; 512 of 256 102 / 167.)
+constexpr int kFewPages = 4096;
 // Shares of fewer items cost more in joins than they save.  (1 unit of 64 pages, 4 / 8 / 16 items: 7.6 / 7.8 / 9.2 us; 64 of 24: 10.9 / 10.2 / 11.6.)
 constexpr int kMinShare = 8;
 // max_items: pages that a sequence can have to be looked at (a window may begin and end inside one)
@@ -673,7 +676,7 @@ int plan_paged(int dtype, int B, int H, int Hk, int head_dim, int max_len, int w
   const long long items = max_sel > 0 ? max_sel : window > 0 && in_window < whole ? in_window : whole;
   const int G = H / Hk;
   const bool bf = dtype == CERB_BF16;
-  g->heads_unit = bf ? (G > 8 ? 16 : 8) : G > 4 ? 8 : G > 2 ? 4 : G;
+  g->heads_unit = bf ? (G > 8 && (long long)B * Hk * ((G + 7) / 8) * items > kFewPages ? 16 : 8) : G > 4 ? 8 : G > 2 ? 4 : G;
   g->units_h = (G + g->heads_unit - 1) / g->heads_unit;
   g->units = (long long)B * Hk * g->units_h;
   if (g->units * std::max(g->heads_unit, PA_CLUSTER) > 0x7fffffffll) return CERB_E_SHAPE;

@@ -243,7 +243,7 @@ def test_attention_of_long_caches_in_splits(dtype, lens, window, hint):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("B,Hk,G,D,longest,window", [(120, 5, 1, 64, 60, 0), (120, 5, 1, 128, 200, 50), (75, 4, 3, 128, 64, 0), (90, 8, 9, 64, 250, 0), (60, 16, 2, 64, 33, 1),
+@pytest.mark.parametrize("B,Hk,G,D,longest,window", [(120, 5, 1, 64, 60, 0), (120, 5, 1, 128, 200, 50), (75, 4, 3, 128, 64, 0), (90, 8, 9, 64, 250, 0), (60, 16, 2, 64, 33, 1), (64, 4, 16, 128, 700, 0), (40, 2, 40, 64, 3000, 500),
                                                      (300, 2, 17, 128, 40, 0)])
 def test_attention_of_many_short_sequences(dtype, B, Hk, G, D, longest, window):
     rng = random.Random(B)
