@@ -13,9 +13,10 @@ namespace cerb {
 namespace {
 
 constexpr int PLAN_THREADS = 1024, PLAN_FEW = 256;
-constexpr int TRIM_CLUSTER = 8;
+constexpr int TRIM_CLUSTER = 8, TRIM_WIDE = 16;      // CTAs of a trim's cluster, of more requests than a CTA has threads
 // Up to this many rows one CTA fills them; more are spread over the SMs, and a second launch changes the state.
-constexpr int kPlanRowsAlone = 4096;
+// (64 requests of a token each: plan and trim 6.0 us; 300 requests, 11000 rows: 9.3; 2000 requests, a million rows, 45000 pages back: 19.)
+constexpr int kPlanRowsAlone = 2048;
 constexpr int kMaxRequests = 8192;      // four words each of a CTA's shared memory
 
 struct PagesParams {
@@ -30,6 +31,17 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 
 __device__ __forceinline__ int pages_of(int tokens) { return (int)(((unsigned)tokens + CERB_PAGE - 1) / CERB_PAGE); }
 
+// Rows and pages, summed up together.
+struct Sums {
+  long long rows;
+  int pages;
+};
+__device__ __forceinline__ Sums operator+(Sums a, Sums b) { return Sums{a.rows + b.rows, a.pages + b.pages}; }
+__device__ __forceinline__ Sums shuffle_up(Sums v, int o) { return Sums{__shfl_up_sync(0xffffffffu, v.rows, o), __shfl_up_sync(0xffffffffu, v.pages, o)}; }
+__device__ __forceinline__ Sums shuffle(Sums v, int i) { return Sums{__shfl_sync(0xffffffffu, v.rows, i), __shfl_sync(0xffffffffu, v.pages, i)}; }
+__device__ __forceinline__ int shuffle_up(int v, int o) { return __shfl_up_sync(0xffffffffu, v, o); }
+__device__ __forceinline__ int shuffle(int v, int i) { return __shfl_sync(0xffffffffu, v, i); }
+
 // Inclusive sum over the CTA's threads; `total` is that of all.
 template <int THREADS, typename T>
 __device__ __forceinline__ T block_scan(T v, T* red, T& total) {
@@ -37,120 +49,163 @@ __device__ __forceinline__ T block_scan(T v, T* red, T& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const T u = __shfl_up_sync(0xffffffffu, v, o);
-    if (lane >= o) v += u;
+    const T u = shuffle_up(v, o);
+    if (lane >= o) v = v + u;
   }
   if (lane == 31) red[warp] = v;
   __syncthreads();
-  T w = lane < WARPS ? red[lane] : 0;
+  T w = lane < WARPS ? red[lane] : T{};
 #pragma unroll
   for (int o = 1; o < WARPS; o <<= 1) {
-    const T u = __shfl_up_sync(0xffffffffu, w, o);
-    if (lane >= o) w += u;
+    const T u = shuffle_up(w, o);
+    if (lane >= o) w = w + u;
   }
-  total = __shfl_sync(0xffffffffu, w, WARPS - 1);
-  const T before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
+  total = shuffle(w, WARPS - 1);
+  const T before = shuffle(w, (warp + 31) & 31);
   __syncthreads();
-  return v + (warp ? before : 0);
+  return warp ? v + before : v;
 }
 
 // The lengths of a request as the kernels use them: what is out of range is taken to the nearest that is in range.
 __device__ __forceinline__ int held_tokens(const PagesParams& p, int b) { return min(max(p.len[b], 0), p.max_pages * CERB_PAGE); }
 
-// The last request that begins at or before item i; ends[b]: first item behind request b.
+// The request that item i is of, ends[b] being the first item behind request b (all lanes of a warp, one item): thirty-two bounds at a time.
 __device__ __forceinline__ int find_request(const int* ends, int B, int i) {
-  int lo = 0, hi = B - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (ends[mid] <= i) lo = mid + 1;
+  const int lane = threadIdx.x & 31;
+  int lo = 0;
+  for (int n = B; n > 1;) {
+    const int step = (n + 31) / 32, at = lo + (lane + 1) * step - 1;
+    const int before = __popc(__ballot_sync(0xffffffffu, at < B && at < lo + n && ends[at] <= i));
+    lo += before * step;
+    n = min(step, B - lo);
+  }
+  return min(lo, B - 1);
+}
+// ... and that of item i, which is of request b or of one of the next 128 with items.  (By a lane.)
+__device__ __forceinline__ int find_near(const int* ends, int B, int b, int i) {
+  int hi = B - 1;
+  while (b < hi) {
+    const int mid = (b + hi) >> 1;
+    if (ends[mid] <= i) b = mid + 1;
     else hi = mid;
   }
-  return lo;
+  return b;
 }
 
-// Two prefix sums over the requests (rows, and pages of those that fit) and then a row per element: its request, position and slot.
+// Prefix sums over the requests (rows, and pages of those that fit) and then a row per element: its request, position and slot.
 // New pages never lie where a row of this call finds an old one, so the table may change at once.  Lengths and free count change when all have read them:
 // with one CTA (ALONE) at its end, with more (each of which sums up for itself) in a launch of their own.
 template <int THREADS, bool ALONE>
 __global__ void __launch_bounds__(THREADS, 1) pages_plan_kernel(const PagesParams p) {
   extern __shared__ __align__(16) int sm[];
   int *ends = sm, *lens = ends + p.B, *base = lens + p.B, *give = base + p.B;     // rows before and of b, length, new pages before, 1 if granted
-  __shared__ long long red_rows[32];
-  __shared__ int red_pages[32], s_taken;
-  const int tid = threadIdx.x;
+  __shared__ Sums red[32];
+  __shared__ int s_taken;
+  const int tid = threadIdx.x, lane = tid & 31;
   const unsigned cta = ALONE ? 0 : blockIdx.x, ctas = ALONE ? 1 : gridDim.x;
   if (tid == 0) s_taken = 0;
   griddep_wait();
   const int n_free = min(max(*p.n_free, 0), p.free_cap);
-  long long rows_before = 0;
-  int pages_before = 0;
+  Sums before{0, 0};
   for (int b0 = 0; b0 < p.B; b0 += THREADS) {
     const int b = b0 + tid;
     const bool live = b < p.B;
     const int len = live ? held_tokens(p, b) : 0, n = live ? max(p.n_new[b], 0) : 0;
-    long long rows_total;
-    const long long end = rows_before + block_scan<THREADS>((long long)n, red_rows, rows_total);
-    const bool fits = live && (long long)len + n <= (long long)p.max_pages * CERB_PAGE && end <= p.rows;
+    // (those that do not fit the rows come last: whatever they add to the pages is added to nobody's)
+    bool fits = live && (long long)len + n <= (long long)p.max_pages * CERB_PAGE;
     const int need = fits ? pages_of(len + n) - pages_of(len) : 0;
-    int pages_total;
-    const int cum = pages_before + block_scan<THREADS>(need, red_pages, pages_total);
-    const bool ok = fits && (need == 0 || cum <= n_free);
+    Sums total;
+    const Sums end = before + block_scan<THREADS>(Sums{n, need}, red, total);
+    fits = fits && end.rows <= p.rows;
+    const bool ok = fits && (need == 0 || end.pages <= n_free);
     if (live) {
-      ends[b] = (int)min(end, 0x7fffffffll);
+      ends[b] = (int)min(end.rows, 0x7fffffffll);
       lens[b] = len;
-      base[b] = cum - need;
+      base[b] = end.pages - need;
       give[b] = ok;
       if (cta == 0) {
         p.granted[b] = ok ? n : 0;
-        p.row_off[b + 1] = (int)min(end, 0x7fffffffll);
+        p.row_off[b + 1] = (int)min(end.rows, 0x7fffffffll);
         // (the ones with new pages that get them are the first ones)
-        if (ALONE && ok && need) atomicMax(&s_taken, cum);
+        if (ALONE && ok && need) atomicMax(&s_taken, end.pages);
       }
     }
-    rows_before += rows_total;
-    pages_before += pages_total;
+    before = before + total;
   }
   if (cta == 0 && tid == 0) p.row_off[0] = 0;
   __syncthreads();
-  const int total = (int)min(rows_before, (long long)p.rows);
-  const bool wide = !(((uintptr_t)p.slot | (uintptr_t)p.pos | (uintptr_t)p.seq) & 15);
-  for (int r0 = 4 * (int)(cta * THREADS + tid); r0 < p.rows; r0 += 4 * (int)(ctas * THREADS)) {
-    int slot[4], pos[4], seq[4];
-    const int32_t* from[4];
-    int32_t* entry[4];
-    int b = r0 < total ? find_request(ends, p.B, r0) : 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = r0 + i;
-      slot[i] = pos[i] = seq[i] = -1;
-      from[i] = nullptr;
-      entry[i] = nullptr;
-      if (r >= total) continue;
-      while (ends[b] <= r) ++b;
-      if (!give[b]) continue;
-      const int first = b ? ends[b - 1] : 0, len = lens[b], at = len + r - first, j = at / CERB_PAGE, held = pages_of(len);
-      int32_t* e = p.page_table + (size_t)b * p.max_pages + j;
-      from[i] = j < held ? e : p.free_pages + (n_free - 1 - base[b] - (j - held));
-      if (j >= held && at % CERB_PAGE == 0) entry[i] = e;
-      pos[i] = at;
-      seq[i] = b;
+  const int total = (int)min(before.rows, (long long)p.rows);
+  // where page j of request b comes from
+  auto source = [&](int b, int j) {
+    const int held = pages_of(lens[b]);
+    return j < held ? p.page_table + (size_t)b * p.max_pages + j : p.free_pages + (n_free - 1 - base[b] - (j - held));
+  };
+  if (ALONE || p.rows <= (int)(ctas * THREADS)) {
+    // a row to a lane: with few rows the time is that of the loads one after another
+    for (int r = (int)(cta * THREADS) + tid; r < p.rows; r += (int)(ctas * THREADS)) {
+      int slot = -1, pos = -1, seq = -1;
+      if (r < total) {
+        const int b = find_near(ends, p.B, 0, r);
+        if (give[b]) {
+          seq = b;
+          pos = lens[b] + r - (b ? ends[b - 1] : 0);
+          const int j = pos / CERB_PAGE, page = *source(b, j);
+          if (pos % CERB_PAGE == 0) p.page_table[(size_t)b * p.max_pages + j] = page;      // (a page that begins here is new)
+          slot = page * CERB_PAGE + pos % CERB_PAGE;
+        }
+      }
+      p.slot[r] = slot;
+      p.pos[r] = pos;
+      p.seq[r] = seq;
     }
+  } else {
+    // four rows to a lane, mostly of one request
+    const bool wide = !(((uintptr_t)p.slot | (uintptr_t)p.pos | (uintptr_t)p.seq) & 15);
+    for (int w0 = 4 * (int)(cta * THREADS + (tid & ~31)); w0 < p.rows; w0 += 4 * (int)(ctas * THREADS)) {
+      const int r0 = w0 + 4 * lane;
+      int slot[4], pos[4], seq[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (from[i]) slot[i] = *from[i];
+      for (int i = 0; i < 4; ++i) slot[i] = pos[i] = seq[i] = -1;
+      int b = w0 < total ? find_request(ends, p.B, w0) : 0;
+      const bool one = w0 + 127 < total && ends[b] > w0 + 127;
+      if (!one && r0 < total) b = find_near(ends, p.B, b, r0);
+      if (one || (r0 + 3 < total && ends[b] > r0 + 3)) {
+        if (give[b]) {
+          const int at = lens[b] + r0 - (b ? ends[b - 1] : 0), j = at / CERB_PAGE;
+          const bool cross = (at + 3) / CERB_PAGE != j;
+          const int32_t* from = source(b, j);
+          const int32_t* from2 = cross ? source(b, j + 1) : from;
+          const int page = *from, page2 = *from2;
+          if (at % CERB_PAGE == 0 || cross) p.page_table[(size_t)b * p.max_pages + j + cross] = page2;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (entry[i]) *entry[i] = slot[i];
-      if (from[i]) slot[i] = slot[i] * CERB_PAGE + pos[i] % CERB_PAGE;
-    }
-    if (wide && r0 + 3 < p.rows) {
-      *reinterpret_cast<int4*>(p.slot + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
-      *reinterpret_cast<int4*>(p.pos + r0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
-      *reinterpret_cast<int4*>(p.seq + r0) = make_int4(seq[0], seq[1], seq[2], seq[3]);
-    } else {
+          for (int i = 0; i < 4; ++i) {
+            pos[i] = at + i;
+            seq[i] = b;
+            slot[i] = ((at + i) / CERB_PAGE == j ? page : page2) * CERB_PAGE + (at + i) % CERB_PAGE;
+          }
+        }
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < 4 && r0 + i < total; ++i) {
+          while (ends[b] <= r0 + i) ++b;
+          if (!give[b]) continue;
+          const int at = lens[b] + r0 + i - (b ? ends[b - 1] : 0), page = *source(b, at / CERB_PAGE);
+          if (at % CERB_PAGE == 0) p.page_table[(size_t)b * p.max_pages + at / CERB_PAGE] = page;
+          const int x = page * CERB_PAGE + at % CERB_PAGE;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (r0 + i < p.rows) { p.slot[r0 + i] = slot[i]; p.pos[r0 + i] = pos[i]; p.seq[r0 + i] = seq[i]; }
+          for (int k = 0; k < 4; ++k)
+            if (k == i) { slot[k] = x; pos[k] = at; seq[k] = b; }
+        }
+      }
+      if (wide && r0 + 3 < p.rows) {
+        *reinterpret_cast<int4*>(p.slot + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+        *reinterpret_cast<int4*>(p.pos + r0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+        *reinterpret_cast<int4*>(p.seq + r0) = make_int4(seq[0], seq[1], seq[2], seq[3]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (r0 + i < p.rows) { p.slot[r0 + i] = slot[i]; p.pos[r0 + i] = pos[i]; p.seq[r0 + i] = seq[i]; }
+      }
     }
   }
   if (!ALONE) return;
@@ -180,7 +235,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) pages_trim_kernel(const Pages
   int *ends = sm, *news = ends + p.B;                          // pages given back before and of b; the length kept
   __shared__ int red_pages[32];
   const int tid = threadIdx.x;
-  const unsigned cta = blockIdx.x;
+  const unsigned cta = blockIdx.x, ctas = gridDim.x;                 // (one cluster)
   griddep_wait();
   const int n_free = min(max(*p.n_free, 0), p.free_cap);
   int total = 0;
@@ -194,24 +249,26 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) pages_trim_kernel(const Pages
   }
   cluster_arrive();
   __syncthreads();
-  for (int i0 = 4 * (int)(cta * PLAN_THREADS + tid); i0 < total; i0 += 4 * TRIM_CLUSTER * PLAN_THREADS) {
-    int32_t* entry[4];
-    int page[4], b = find_request(ends, p.B, i0);
+  // two pages to a lane
+  for (int w0 = 2 * (int)(cta * PLAN_THREADS + (tid & ~31)); w0 < total; w0 += 2 * (int)(ctas * PLAN_THREADS)) {
+    int b = find_request(ends, p.B, w0), page[2];
+    int32_t* entry[2] = {nullptr, nullptr};
+    const bool one = ends[b] > w0 + 63;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      entry[i] = nullptr;
-      if (i0 + i >= total) continue;
-      while (ends[b] <= i0 + i) ++b;
-      entry[i] = p.page_table + (size_t)b * p.max_pages + pages_of(news[b]) + i0 + i - (b ? ends[b - 1] : 0);
+    for (int i = 0; i < 2; ++i) {
+      const int at = w0 + 32 * i + (tid & 31);
+      if (at >= total) continue;
+      const int c = one ? b : find_near(ends, p.B, b, at);
+      entry[i] = p.page_table + (size_t)c * p.max_pages + pages_of(news[c]) + at - (c ? ends[c - 1] : 0);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 2; ++i)
       if (entry[i]) page[i] = *entry[i];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 2; ++i)
       if (entry[i]) {
-        const int at = n_free + total - 1 - i0 - i;
-        if (at < p.free_cap) p.free_pages[at] = page[i];
+        const int to = n_free + total - 1 - (w0 + 32 * i + (tid & 31));
+        if (to < p.free_cap) p.free_pages[to] = page[i];
         *entry[i] = -1;
       }
   }
@@ -375,14 +432,14 @@ int cerb_pages_plan(const cerb_pages* s, const int32_t* n_new, int32_t rows, int
   const size_t smem = 4 * (size_t)p.B * sizeof(int);
   cudaStream_t st = (cudaStream_t)stream;
   static std::atomic<uint64_t> done[2];
-  if (p.B <= PLAN_FEW && rows <= 4 * PLAN_FEW)
+  if (p.B <= PLAN_FEW && rows <= 2 * PLAN_FEW)
     return launch_pdl(pages_plan_kernel<PLAN_FEW, true>, dim3(1), dim3(PLAN_FEW), smem, st, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
   if (rows <= kPlanRowsAlone) {
     CERB_TRY(allow_smem(pages_plan_kernel<PLAN_THREADS, true>, done[0], 4 * kMaxRequests * (int)sizeof(int)));
     return launch_pdl(pages_plan_kernel<PLAN_THREADS, true>, dim3(1), dim3(PLAN_THREADS), smem, st, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
   }
   CERB_TRY(allow_smem(pages_plan_kernel<PLAN_THREADS, false>, done[1], 4 * kMaxRequests * (int)sizeof(int)));
-  const int ctas = std::min(148, (rows + 4 * PLAN_THREADS - 1) / (4 * PLAN_THREADS));
+  const int ctas = std::min(148, (rows + PLAN_THREADS - 1) / PLAN_THREADS);
   if (launch_pdl(pages_plan_kernel<PLAN_THREADS, false>, dim3((unsigned)ctas), dim3(PLAN_THREADS), smem, st, p) != cudaSuccess) return CERB_E_CUDA;
   return launch_pdl(pages_grant_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
 }
@@ -393,10 +450,12 @@ int cerb_pages_trim(const cerb_pages* s, const int32_t* keep, void* stream) {
   if (!keep) return CERB_E_ARG;
   PagesParams p = pages_params(s);
   p.n_new = keep;
-  static std::atomic<uint64_t> done{0};
-  CERB_TRY(allow_smem(pages_trim_kernel, done, 2 * kMaxRequests * (int)sizeof(int)));
-  return launch_pdl_cluster(pages_trim_kernel, dim3(TRIM_CLUSTER), dim3(PLAN_THREADS), 2 * (size_t)p.B * sizeof(int), (cudaStream_t)stream,
-                            TRIM_CLUSTER, p) == cudaSuccess ? CERB_OK : CERB_E_CUDA;
+  static std::atomic<uint64_t> done[2];
+  CERB_TRY(allow_smem(pages_trim_kernel, done[0], 2 * kMaxRequests * (int)sizeof(int)));
+  const unsigned ctas = p.B > PLAN_THREADS ? TRIM_WIDE : TRIM_CLUSTER;
+  if (ctas > 8) CERB_TRY(allow_wide_clusters(pages_trim_kernel, done[1]));
+  return launch_pdl_cluster(pages_trim_kernel, dim3(ctas), dim3(PLAN_THREADS), 2 * (size_t)p.B * sizeof(int), (cudaStream_t)stream, ctas, p) == cudaSuccess
+             ? CERB_OK : CERB_E_CUDA;
 }
 
 int cerb_kv_append(const cerb_kv_append_args* a, void* stream) {
