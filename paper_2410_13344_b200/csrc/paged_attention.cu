@@ -69,34 +69,52 @@ __device__ __forceinline__ PageRef page_ref(const PagedParams& p, int first, int
   return r;
 }
 
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
 // The running maxima, sums and unnormalised outputs of a CTA's warps.
 template <int DH, int HEADS>
 struct alignas(16) Sums {                                                // (written and sent in pieces of 8 bytes)
   float o[PA_WARPS][HEADS][DH], m[PA_WARPS][HEADS], l[PA_WARPS][HEADS];
 };
+// Four columns of a head from d on, with its maximum and sum.
 template <int DH, int HEADS>
-__device__ __forceinline__ float merge_warps(const Sums<DH, HEADS>& s, int h, int d, float& m, float& l) {
+__device__ __forceinline__ float4 merge_warps(const Sums<DH, HEADS>& s, int h, int d, float& m, float& l) {
+  float f[PA_WARPS];
   m = -INFINITY;
 #pragma unroll
   for (int w = 0; w < PA_WARPS; ++w) m = fmaxf(m, s.m[w][h]);
   const float u = m == -INFINITY ? 0.f : m;
-  float o = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   l = 0.f;
 #pragma unroll
   for (int w = 0; w < PA_WARPS; ++w) {
-    const float f = exp2f(s.m[w][h] - u);
-    l += s.l[w][h] * f;
-    o += s.o[w][h][d] * f;
+    f[w] = exp2f(s.m[w][h] - u);
+    l += s.l[w][h] * f[w];
+    const float4 x = *reinterpret_cast<const float4*>(&s.o[w][h][d]);
+    o = make_float4(o.x + x.x * f[w], o.y + x.y * f[w], o.z + x.z * f[w], o.w + x.w * f[w]);
   }
   return o;
 }
-// (a row without keys: zeros, and the logarithm of nothing)
+// What a sum of weights is divided by, as a factor.  (A row without keys: zeros; its lse is the logarithm of nothing.)
+__device__ __forceinline__ float one_over(float l) { return l > 0.f || l != l ? 1.f / l : 0.f; }
 template <typename T>
-__device__ __forceinline__ void store_out(const PagedParams& p, size_t row, int d, int dh, float o, float m, float l) {
-  const float x = l > 0.f || l != l ? o / l : 0.f;
+__device__ __forceinline__ void store_out(const PagedParams& p, size_t row, int d, int dh, float x) {
   if constexpr (sizeof(T) == 2) reinterpret_cast<bf16*>(p.out)[row * dh + d] = __float2bfloat16_rn(x);
   else reinterpret_cast<float*>(p.out)[row * dh + d] = x;
-  if (d == 0 && p.lse) p.lse[row] = (m + log2f(l)) * kLn2;
+}
+template <typename T>
+__device__ __forceinline__ void store_out(const PagedParams& p, size_t row, int d, int dh, float4 x) {
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(p.out) + row * dh + d) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+  else
+    *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + row * dh + d) = x;
+}
+__device__ __forceinline__ void store_lse(const PagedParams& p, size_t row, float m, float l) {
+  if (p.lse) p.lse[row] = (m + log2f(l)) * kLn2;
 }
 
 // A piece of a unit: the items from item0 up to item1, of which a warp takes every stride-th, for these of the query heads.
@@ -129,11 +147,6 @@ struct Walk {
   }
 };
 
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a));
@@ -452,7 +465,8 @@ __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_
   // sequences without anything to look at
   for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
     if (span_of(p, b).items) continue;
-    for (int i = threadIdx.x; i < p.H * DH; i += PA_WARPS * 32) store_out<T>(p, (size_t)b * p.H + i / DH, i % DH, DH, 0.f, -INFINITY, 0.f);
+    for (int i = threadIdx.x; i < p.H * DH; i += PA_WARPS * 32) store_out<T>(p, (size_t)b * p.H + i / DH, i % DH, DH, 0.f);
+    for (int i = threadIdx.x; i < p.H; i += PA_WARPS * 32) store_lse(p, (size_t)b * p.H + i, -INFINITY, 0.f);
     if (p.by_unit)
       for (int i = threadIdx.x; i < uh; i += PA_WARPS * 32) p.meta[b * uh + i] = make_int4(0, 0, 0, 0);
   }
@@ -487,16 +501,19 @@ __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_
     }
     attend<T, DH, HEADS>(p, c, sums);
     __syncthreads();
-    for (int i = threadIdx.x; i < c.heads * DH; i += PA_WARPS * 32) {
+    for (int i = 4 * threadIdx.x; i < c.heads * DH; i += 4 * PA_WARPS * 32) {
       const int h = i / DH, d = i % DH;
       float m, l;
-      const float o = merge_warps(sums, h, d, m, l);
+      const float4 o = merge_warps(sums, h, d, m, l);
       if (n < items) {
         const size_t to = (size_t)slot * HEADS + h;
-        p.part_o[to * DH + d] = o;
-        if (d == 0) { p.part_ml[2 * to] = m; p.part_ml[2 * to + 1] = l; }
+        *reinterpret_cast<float4*>(p.part_o + to * DH + d) = o;
+        if (d == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * to) = make_float2(m, l);
       } else {
-        store_out<T>(p, (size_t)c.b * p.H + c.head0 + h, d, DH, o, m, l);
+        const float r = one_over(l);
+        const size_t row = (size_t)c.b * p.H + c.head0 + h;
+        store_out<T>(p, row, d, DH, make_float4(o.x * r, o.y * r, o.z * r, o.w * r));
+        if (d == 0) store_lse(p, row, m, l);
       }
     }
     __syncthreads();
@@ -511,7 +528,8 @@ template <typename T, int DH, int HEADS>
 __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_attn_cluster_kernel(const PagedParams p) {
   __shared__ Sums<DH, HEADS> sums;
   __shared__ alignas(16) float s_o[HEADS * DH];                          // [CTA][its part of the outputs]
-  __shared__ alignas(16) float2 s_ml[PA_CLUSTER][HEADS];
+  __shared__ alignas(16) float2 s_ml[HEADS][PA_CLUSTER];
+  __shared__ float s_f[PA_CLUSTER][HEADS];                               // weight of a CTA's sums in a head's result
   const int n = p.together, rank = blockIdx.x % n, unit = blockIdx.x / n;
   cluster_start_arrive();
   const int part = unit % p.units_h;
@@ -533,29 +551,41 @@ __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_
   attend<T, DH, HEADS>(p, c, sums);
   __syncthreads();
   cluster_start_wait();                                                  // every CTA of the cluster runs
-  for (int i = threadIdx.x; i < c.heads * DH; i += PA_WARPS * 32) {
+  for (int i = 4 * threadIdx.x; i < c.heads * DH; i += 4 * PA_WARPS * 32) {
     float m, l;
-    const float o = merge_warps(sums, i / DH, i % DH, m, l);
-    const int to = i / own;
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa_u32(smem_u32(&s_o[rank * own + i - to * own]), to)), "f"(o) : "memory");
+    const int h = i / DH, d = i % DH, to = i / own;                      // (a CTA's part of the outputs is a multiple of four columns)
+    const float4 o = merge_warps(sums, h, d, m, l);
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(mapa_u32(smem_u32(&s_o[rank * own + i - to * own]), to)), "f"(o.x), "f"(o.y), "f"(o.z),
+                 "f"(o.w) : "memory");
     // (the maximum and the sum of a head: to all, one each from the threads of its first columns)
-    if (i % DH < n)
-      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(mapa_u32(smem_u32(&s_ml[rank][i / DH]), i % DH)), "f"(m), "f"(l) : "memory");
+    if (d / 4 < n)
+      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(mapa_u32(smem_u32(&s_ml[h][rank]), d / 4)), "f"(m), "f"(l) : "memory");
   }
   cluster_start_arrive();
   cluster_start_wait();                                                  // ... and has sent its sums
+  // the heads of this CTA's part, a CTA of the cluster to a lane
+  const int h0 = rank * own / DH, h1 = min(c.heads, (rank * own + own - 1) / DH + 1);
+  for (int h = h0 + (threadIdx.x >> 5); h < h1; h += PA_WARPS) {
+    const int lane = threadIdx.x & 31;
+    const float2 x = lane < n ? s_ml[h][lane] : make_float2(-INFINITY, 0.f);
+    float m = x.x;
+#pragma unroll
+    for (int w = PA_CLUSTER / 2; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
+    const float f = exp2f(x.x - (m == -INFINITY ? 0.f : m));
+    float l = x.y * f;
+#pragma unroll
+    for (int w = PA_CLUSTER / 2; w > 0; w >>= 1) l += __shfl_xor_sync(0xffffffffu, l, w);
+    if (lane < n) s_f[lane][h] = f * one_over(l);
+    if (lane == 0 && rank * own <= h * DH) store_lse(p, (size_t)c.b * p.H + c.head0 + h, m, l);
+  }
+  __syncthreads();
   for (int j = threadIdx.x; j < own; j += PA_WARPS * 32) {
     const int i = rank * own + j, h = i / DH;
     if (h >= c.heads) break;
-    float m = -INFINITY, l = 0.f, o = 0.f;
-    for (int r = 0; r < n; ++r) m = fmaxf(m, s_ml[r][h].x);
-    const float u = m == -INFINITY ? 0.f : m;
-    for (int r = 0; r < n; ++r) {
-      const float f = exp2f(s_ml[r][h].x - u);
-      l += s_ml[r][h].y * f;
-      o += s_o[r * own + j] * f;
-    }
-    store_out<T>(p, (size_t)c.b * p.H + c.head0 + h, i % DH, DH, o, m, l);
+    float o = 0.f;
+#pragma unroll 4
+    for (int r = 0; r < n; ++r) o = fmaf(s_f[r][h], s_o[r * own + j], o);
+    store_out<T>(p, (size_t)c.b * p.H + c.head0 + h, i % DH, DH, o);
   }
 }
 
@@ -583,9 +613,13 @@ __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_
   c.item1 = c.sp.items;
   attend<T, DH, HEADS>(p, c, sums);
   __syncwarp();
-  for (int i = lane; i < c.heads * DH; i += 32) {
+  for (int i = 4 * lane; i < c.heads * DH; i += 4 * 32) {
     const int h = i / DH, d = i % DH;
-    store_out<T>(p, (size_t)c.b * p.H + c.head0 + h, d, DH, sums.o[warp][h][d], sums.m[warp][h], sums.l[warp][h]);
+    const size_t row = (size_t)c.b * p.H + c.head0 + h;
+    const float4 o = *reinterpret_cast<const float4*>(&sums.o[warp][h][d]);
+    const float r = one_over(sums.l[warp][h]);
+    store_out<T>(p, row, d, DH, make_float4(o.x * r, o.y * r, o.z * r, o.w * r));
+    if (d == 0) store_lse(p, row, sums.m[warp][h], sums.l[warp][h]);
   }
 }
 
@@ -644,8 +678,10 @@ __global__ void __launch_bounds__(1024) paged_join_kernel(const PagedParams p, i
   }
   if (!live) return;
   const size_t row = (size_t)b * p.H + kvh * p.G + part * heads_unit + h;
+  const float r = one_over(l);
 #pragma unroll
-  for (int e = 0; e < E; ++e) store_out<T>(p, row, lane * E + e, DH, o.x[e], m, l);
+  for (int e = 0; e < E; ++e) store_out<T>(p, row, lane * E + e, DH, o.x[e] * r);
+  if (lane == 0) store_lse(p, row, m, l);
 }
 
 // How a call is cut up: heads of a unit, units of a KV head, CTAs (and of them in a cluster, 0: shares and a join).
@@ -753,7 +789,7 @@ int cerb_paged_attention(const cerb_paged_attn_args* a, void* stream) {
   CERB_TRY(plan_paged(a->dtype, a->B, a->n_heads, a->n_kv_heads, a->head_dim, a->max_len, a->window, max_sel, &g));
   const int es = a->dtype == CERB_BF16 ? 2 : 4;
   if (a->q_row_stride * es % 16 || a->q_head_stride * es % 16) return CERB_E_ARG;
-  if (((uintptr_t)a->q | (uintptr_t)a->k_pool | (uintptr_t)a->v_pool | (uintptr_t)a->scratch) & 15) return CERB_E_ARG;
+  if (((uintptr_t)a->q | (uintptr_t)a->k_pool | (uintptr_t)a->v_pool | (uintptr_t)a->out | (uintptr_t)a->scratch) & 15) return CERB_E_ARG;
   const size_t need = scratch_bytes(g, a->head_dim);
   if (need > a->scratch_bytes || (need && !a->scratch)) return CERB_E_NOMEM;
   if (a->B == 0) return CERB_OK;

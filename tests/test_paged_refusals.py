@@ -123,7 +123,7 @@ def test_attention_refusals():
     assert call(**none) == binding.OK
     for name in ("q", "k_pool", "v_pool", "page_table", "len", "out"):
         assert call(**{name: None}) == binding.E_ARG, name
-    for name in ("q", "k_pool", "v_pool"):
+    for name in ("q", "k_pool", "v_pool", "out"):
         assert call(**{name: AT + 8}) == binding.E_ARG, name
     for name in ("q_row_stride", "q_head_stride"):
         assert call(**{name: 68}) == binding.E_ARG, name
