@@ -160,8 +160,8 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
 // interleaved into fragments by byte permutes.  S^T's sums become P^T's fragments by 8 x 8 transpositions of 16-bit elements.
 // P is rounded to bf16 for the second product (each weight off by at most 2^-8 of itself, up or down; the sum l is that of the unrounded
 // ones); scores, maxima, sums and outputs are fp32.
-// A warp takes KP pages at a time, 8 KB of keys and values, and has the next ones on their way.
-template <int DH, int NT>
+// A warp takes KP pages at a time, 8 KB of keys and values, and has the next AHEAD times as many on their way.
+template <int DH, int NT, int AHEAD>
 __device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c, Sums<DH, 8 * NT>& sums) {
   constexpr int KC = DH / 32, VH = DH / 64, KP = 128 / DH;               // chunks of a key row, halves of a value row, pages at a time
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -169,11 +169,8 @@ __device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c
   const bf16* vp = reinterpret_cast<const bf16*>(p.v_pool) + (size_t)c.kvh * CERB_PAGE * DH + 2 * t * DH + g * 8;
   const size_t page_elems = (size_t)p.Hk * CERB_PAGE * DH;
   Walk walk(c);
-  PageRef now[KP], then[KP];
-#pragma unroll
-  for (int a = 0; a < KP; ++a) now[a] = walk.next(p, c);
-  uint4 k[KP][2][KC], v[KP][4][VH];
-  auto load_k = [&](const PageRef (&r)[KP]) {
+  uint4 kk[AHEAD][KP][2][KC], vv[AHEAD][KP][4][VH];
+  auto load_k = [&](uint4 (&k)[KP][2][KC], const PageRef (&r)[KP]) {
 #pragma unroll
     for (int a = 0; a < KP; ++a)
 #pragma unroll
@@ -181,7 +178,7 @@ __device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c
 #pragma unroll
         for (int j = 0; j < KC; ++j) k[a][e][j] = KP == 1 || r[a].at >= 0 ? ld16(kp + r[a].at * page_elems + e * 8 * DH + 32 * j) : make_uint4(0, 0, 0, 0);
   };
-  auto load_v = [&](const PageRef (&r)[KP]) {
+  auto load_v = [&](uint4 (&v)[KP][4][VH], const PageRef (&r)[KP]) {
 #pragma unroll
     for (int a = 0; a < KP; ++a)
 #pragma unroll
@@ -190,7 +187,13 @@ __device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c
         for (int j = 0; j < VH; ++j)
           v[a][e][j] = KP == 1 || r[a].at >= 0 ? ld16(vp + r[a].at * page_elems + ((e & 1) + 8 * (e >> 1)) * DH + 64 * j) : make_uint4(0, 0, 0, 0);
   };
-  if (now[0].at >= 0) { load_k(now); load_v(now); }
+  PageRef ahead[AHEAD][KP];
+#pragma unroll
+  for (int x = 0; x < AHEAD; ++x) {
+#pragma unroll
+    for (int a = 0; a < KP; ++a) ahead[x][a] = walk.next(p, c);
+    if (ahead[x][0].at >= 0) { load_k(kk[x], ahead[x]); load_v(vv[x], ahead[x]); }
+  }
   uint4 q[NT][KC];
 #pragma unroll
   for (int n = 0; n < NT; ++n)
@@ -209,102 +212,110 @@ __device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[n][d][e] = 0.f;
   }
-  while (now[0].at >= 0) {
+  while (ahead[0][0].at >= 0) {
 #pragma unroll
-    for (int a = 0; a < KP; ++a) then[a] = walk.next(p, c);
-    float s[KP][NT][4];
+    for (int x = 0; x < AHEAD; ++x) {
+      PageRef (&now)[KP] = ahead[x];
+      uint4 (&k)[KP][2][KC] = kk[x];
+      uint4 (&v)[KP][4][VH] = vv[x];
+      if (now[0].at < 0) break;                                            // (and none behind it)
+      PageRef then[KP];
 #pragma unroll
-    for (int a = 0; a < KP; ++a)
+      for (int a = 0; a < KP; ++a) then[a] = walk.next(p, c);
+      float s[KP][NT][4];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        // (two accumulators: the tensor cores cut a sum off at every step)
-        float a0[4] = {0.f, 0.f, 0.f, 0.f}, a1[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int a = 0; a < KP; ++a)
 #pragma unroll
-        for (int j = 0; j < KC; ++j) {
-          mma_16816(a0, k[a][0][j].x, k[a][1][j].x, k[a][0][j].y, k[a][1][j].y, q[n][j].x, q[n][j].y);
-          mma_16816(a1, k[a][0][j].z, k[a][1][j].z, k[a][0][j].w, k[a][1][j].w, q[n][j].z, q[n][j].w);
-        }
+        for (int n = 0; n < NT; ++n) {
+          // (two accumulators: the tensor cores cut a sum off at every step)
+          float a0[4] = {0.f, 0.f, 0.f, 0.f}, a1[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[a][n][e] = (a0[e] + a1[e]) * p.scale_log2;
-      }
-    if (then[0].at >= 0) load_k(then);
-#pragma unroll
-    for (int a = 0; a < KP; ++a) {
-      const int row0 = now[a].at >= 0 ? now[a].page * CERB_PAGE : c.sp.hi;
-      if (row0 < c.sp.lo || row0 + CERB_PAGE > c.sp.hi) {
-        // the ends: whatever lies outside counts nothing, and is nothing (it may be infinite)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = row0 + g + 8 * (e >> 1);
-            if (r < c.sp.lo || r >= c.sp.hi) s[a][n][e] = -INFINITY;
+          for (int j = 0; j < KC; ++j) {
+            mma_16816(a0, k[a][0][j].x, k[a][1][j].x, k[a][0][j].y, k[a][1][j].y, q[n][j].x, q[n][j].y);
+            mma_16816(a1, k[a][0][j].z, k[a][1][j].z, k[a][0][j].w, k[a][1][j].w, q[n][j].z, q[n][j].w);
           }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = row0 + 2 * t + (e & 1) + 8 * (e >> 1);
-          if (r < c.sp.lo || r >= c.sp.hi)
-#pragma unroll
-            for (int j = 0; j < VH; ++j) v[a][e][j] = make_uint4(0, 0, 0, 0);
+          for (int e = 0; e < 4; ++e) s[a][n][e] = (a0[e] + a1[e]) * p.scale_log2;
         }
-      }
-    }
-    uint32_t pb[KP][NT][2];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      float mx[2] = {fmaxf(s[0][n][0], s[0][n][2]), fmaxf(s[0][n][1], s[0][n][3])};
-#pragma unroll
-      for (int a = 1; a < KP; ++a)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) mx[e] = fmaxf(mx[e], fmaxf(s[a][n][e], s[a][n][e + 2]));
-#pragma unroll
-      for (int w = 4; w < 32; w <<= 1)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], w));
-      float f[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        mx[e] = fmaxf(mx[e], m[n][e]);
-        const float u = mx[e] == -INFINITY ? 0.f : mx[e];
-        f[e] = exp2f(m[n][e] - u);
-        m[n][e] = mx[e];
-        l[n][e] *= f[e];
-#pragma unroll
-        for (int a = 0; a < KP; ++a) {
-          s[a][n][e] = exp2f(s[a][n][e] - u);
-          s[a][n][e + 2] = exp2f(s[a][n][e + 2] - u);
-          l[n][e] += s[a][n][e] + s[a][n][e + 2];
-        }
-      }
-      if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
-#pragma unroll
-        for (int d = 0; d < 4 * VH; ++d)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[n][d][e] *= f[e & 1];
-      }
+      if (then[0].at >= 0) load_k(k, then);
 #pragma unroll
       for (int a = 0; a < KP; ++a) {
-        pb[a][n][0] = transpose8x8(pack_bf16(s[a][n][0], s[a][n][1]));
-        pb[a][n][1] = transpose8x8(pack_bf16(s[a][n][2], s[a][n][3]));
-      }
-    }
+        const int row0 = now[a].at >= 0 ? now[a].page * CERB_PAGE : c.sp.hi;
+        if (row0 < c.sp.lo || row0 + CERB_PAGE > c.sp.hi) {
+          // the ends: whatever lies outside counts nothing, and is nothing (it may be infinite)
 #pragma unroll
-    for (int a = 0; a < KP; ++a)
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int j = 0; j < VH; ++j) {
-        const uint32_t x[4][4] = {{v[a][0][j].x, v[a][0][j].y, v[a][0][j].z, v[a][0][j].w}, {v[a][1][j].x, v[a][1][j].y, v[a][1][j].z, v[a][1][j].w},
-                                  {v[a][2][j].x, v[a][2][j].y, v[a][2][j].z, v[a][2][j].w}, {v[a][3][j].x, v[a][3][j].y, v[a][3][j].z, v[a][3][j].w}};
+            for (int e = 0; e < 4; ++e) {
+              const int r = row0 + g + 8 * (e >> 1);
+              if (r < c.sp.lo || r >= c.sp.hi) s[a][n][e] = -INFINITY;
+            }
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          const uint32_t a0 = __byte_perm(x[0][d], x[1][d], 0x5410), a1 = __byte_perm(x[0][d], x[1][d], 0x7632);
-          const uint32_t a2 = __byte_perm(x[2][d], x[3][d], 0x5410), a3 = __byte_perm(x[2][d], x[3][d], 0x7632);
+          for (int e = 0; e < 4; ++e) {
+            const int r = row0 + 2 * t + (e & 1) + 8 * (e >> 1);
+            if (r < c.sp.lo || r >= c.sp.hi)
 #pragma unroll
-          for (int n = 0; n < NT; ++n) mma_16816(o[n][4 * j + d], a0, a1, a2, a3, pb[a][n][0], pb[a][n][1]);
+              for (int j = 0; j < VH; ++j) v[a][e][j] = make_uint4(0, 0, 0, 0);
+          }
         }
       }
-    if (then[0].at >= 0) load_v(then);
+      uint32_t pb[KP][NT][2];
 #pragma unroll
-    for (int a = 0; a < KP; ++a) now[a] = then[a];
+      for (int n = 0; n < NT; ++n) {
+        float mx[2] = {fmaxf(s[0][n][0], s[0][n][2]), fmaxf(s[0][n][1], s[0][n][3])};
+#pragma unroll
+        for (int a = 1; a < KP; ++a)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) mx[e] = fmaxf(mx[e], fmaxf(s[a][n][e], s[a][n][e + 2]));
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], w));
+        float f[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          mx[e] = fmaxf(mx[e], m[n][e]);
+          const float u = mx[e] == -INFINITY ? 0.f : mx[e];
+          f[e] = exp2f(m[n][e] - u);
+          m[n][e] = mx[e];
+          l[n][e] *= f[e];
+#pragma unroll
+          for (int a = 0; a < KP; ++a) {
+            s[a][n][e] = exp2f(s[a][n][e] - u);
+            s[a][n][e + 2] = exp2f(s[a][n][e + 2] - u);
+            l[n][e] += s[a][n][e] + s[a][n][e + 2];
+          }
+        }
+        if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
+#pragma unroll
+          for (int d = 0; d < 4 * VH; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[n][d][e] *= f[e & 1];
+        }
+#pragma unroll
+        for (int a = 0; a < KP; ++a) {
+          pb[a][n][0] = transpose8x8(pack_bf16(s[a][n][0], s[a][n][1]));
+          pb[a][n][1] = transpose8x8(pack_bf16(s[a][n][2], s[a][n][3]));
+        }
+      }
+#pragma unroll
+      for (int a = 0; a < KP; ++a)
+#pragma unroll
+        for (int j = 0; j < VH; ++j) {
+          const uint32_t x[4][4] = {{v[a][0][j].x, v[a][0][j].y, v[a][0][j].z, v[a][0][j].w}, {v[a][1][j].x, v[a][1][j].y, v[a][1][j].z, v[a][1][j].w},
+                                    {v[a][2][j].x, v[a][2][j].y, v[a][2][j].z, v[a][2][j].w}, {v[a][3][j].x, v[a][3][j].y, v[a][3][j].z, v[a][3][j].w}};
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const uint32_t a0 = __byte_perm(x[0][d], x[1][d], 0x5410), a1 = __byte_perm(x[0][d], x[1][d], 0x7632);
+            const uint32_t a2 = __byte_perm(x[2][d], x[3][d], 0x5410), a3 = __byte_perm(x[2][d], x[3][d], 0x7632);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma_16816(o[n][4 * j + d], a0, a1, a2, a3, pb[a][n][0], pb[a][n][1]);
+          }
+        }
+      if (then[0].at >= 0) load_v(v, then);
+#pragma unroll
+      for (int a = 0; a < KP; ++a) now[a] = then[a];
+    }
   }
 #pragma unroll
   for (int n = 0; n < NT; ++n)
@@ -444,9 +455,9 @@ __device__ __forceinline__ void attend_f32(const PagedParams& p, const Piece& c,
 }
 
 
-template <typename T, int DH, int HEADS>
+template <typename T, int DH, int HEADS, int AHEAD = 1>
 __device__ __forceinline__ void attend(const PagedParams& p, const Piece& c, Sums<DH, HEADS>& sums) {
-  if constexpr (sizeof(T) == 2) attend_bf16<DH, HEADS / 8>(p, c, sums);
+  if constexpr (sizeof(T) == 2) attend_bf16<DH, HEADS / 8, AHEAD>(p, c, sums);
   else attend_f32<DH, HEADS>(p, c, sums);
 }
 
@@ -524,8 +535,8 @@ __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_
 }
 
 // Every unit a cluster, which meets in its CTAs' shared memory: each CTA joins a part of the outputs, sent to it by all.
-template <typename T, int DH, int HEADS>
-__global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_attn_cluster_kernel(const PagedParams p) {
+template <typename T, int DH, int HEADS, int AHEAD>
+__global__ void __launch_bounds__(PA_WARPS * 32, AHEAD == 1 ? ctas_per_sm<T, HEADS>() : 2) paged_attn_cluster_kernel(const PagedParams p) {
   __shared__ Sums<DH, HEADS> sums;
   __shared__ alignas(16) float s_o[HEADS * DH];                          // [CTA][its part of the outputs]
   __shared__ alignas(16) float2 s_ml[HEADS][PA_CLUSTER];
@@ -548,7 +559,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_
   if (p.window > 0 && !p.sel) c.ahead = page_ref(p, c.sp.first, c.b, c.kvh, warp_item(c, threadIdx.x & 31));
   c.item1 = c.sp.items;
   const int own = HEADS * DH / n;
-  attend<T, DH, HEADS>(p, c, sums);
+  attend<T, DH, HEADS, AHEAD>(p, c, sums);
   __syncthreads();
   cluster_start_wait();                                                  // every CTA of the cluster runs
   for (int i = 4 * threadIdx.x; i < c.heads * DH; i += 4 * PA_WARPS * 32) {
@@ -687,6 +698,7 @@ __global__ void __launch_bounds__(1024) paged_join_kernel(const PagedParams p, i
 // How a call is cut up: heads of a unit, units of a KV head, CTAs (and of them in a cluster, 0: shares and a join).
 struct PagedPlan {
   int heads_unit, units_h, ctas, min_share, joins, together;          // together: -1 a warp per unit
+  bool deep;                                                             // two pages of a warp ahead, in a cluster
   long long units;
 };
 // A cluster per unit, as many CTAs as make the grid one wave and find a page for each of their warps, while the longest sequence leaves a warp no more than 12 pages;
@@ -702,6 +714,9 @@ constexpr int kWarpPages = 4;
 // Groups of more than eight heads in bf16: sixteen to a unit, which reads keys and values once for them; eight, and more CTAs, while those are no more pages than these in all.  (Heads of
 // 128, us with 16 / 8: 2 units of 256 pages 8.5 / 7.0, 32 of 64 14.0 / 8.4, 512 of 4 12.6 / 8.7; 32 of 256 19.9 / 17.0, ragged 11.9 / 15.6; 128 of 64 12.1 / 18.4; 512 of 256 102 / 167.)
 constexpr int kFewPages = 4096;
+// While two CTAs to an SM are enough (and a warp has more than one page), a cluster's warps have the registers for two pages ahead.  (64 units of 32 / 64 pages 8.0 / 10.3 -> 6.6 / 8.4 us, 128
+// of 32 / 64 10.5 / 16.7 -> 9.0 / 14.5.  In shares, and with fewer CTAs to have them so: no gain.)
+
 // Shares of fewer items cost more in joins than they save.  (1 unit of 64 pages, 4 / 8 / 16 items: 7.6 / 7.8 / 9.2 us; 64 of 24: 10.9 / 10.2 / 11.6.)
 constexpr int kMinShare = 8;
 // max_items: pages that a sequence can have to be looked at (a window may begin and end inside one)
@@ -731,6 +746,7 @@ int plan_paged(int dtype, int B, int H, int Hk, int head_dim, int max_len, int w
   if (g->together) {
     g->ctas = (int)g->units * g->together;
     g->joins = 0;
+    g->deep = bf && g->ctas <= 2 * 148 && items > g->together * PA_WARPS * (128 / head_dim);
     return CERB_OK;
   }
   const long long most = std::max(1ll, (g->units * items + g->min_share - 1) / g->min_share);
@@ -744,15 +760,24 @@ size_t scratch_bytes(const PagedPlan& g, int head_dim) {
   return g.units && !g.together ? meta_bytes(g) + part_ml_bytes(g) + (size_t)2 * g.ctas * g.heads_unit * head_dim * sizeof(float) : 0;
 }
 
+template <typename T, int DH, int HEADS, int AHEAD>
+cudaError_t launch_cluster(const PagedPlan& g, const PagedParams& p, cudaStream_t st) {
+  auto kern = paged_attn_cluster_kernel<T, DH, HEADS, AHEAD>;
+  if (g.together > 8) {
+    static std::atomic<uint64_t> done{0};
+    if (allow_wide_clusters(kern, done) != CERB_OK) return cudaErrorInvalidValue;
+  }
+  return launch_pdl_cluster(kern, dim3((unsigned)g.ctas), dim3(PA_WARPS * 32), 0, st, (unsigned)g.together, p);
+}
+
 template <typename T, int DH, int HEADS>
 cudaError_t launch(const PagedPlan& g, const PagedParams& p, cudaStream_t st) {
   const dim3 block(PA_WARPS * 32);
-  if (g.together > 8) {
-    static std::atomic<uint64_t> done{0};
-    if (allow_wide_clusters(paged_attn_cluster_kernel<T, DH, HEADS>, done) != CERB_OK) return cudaErrorInvalidValue;
-  }
   if (g.together < 0) return launch_pdl(paged_attn_warp_kernel<T, DH, HEADS>, dim3((unsigned)g.ctas), block, 0, st, p);
-  if (g.together) return launch_pdl_cluster(paged_attn_cluster_kernel<T, DH, HEADS>, dim3((unsigned)g.ctas), block, 0, st, (unsigned)g.together, p);
+  if (g.together) {
+    constexpr bool deep = sizeof(T) == 2 && HEADS == 8;
+    return deep && g.deep ? launch_cluster<T, DH, HEADS, deep ? 2 : 1>(g, p, st) : launch_cluster<T, DH, HEADS, 1>(g, p, st);
+  }
   const cudaError_t rc = launch_pdl(paged_attn_kernel<T, DH, HEADS>, dim3((unsigned)g.ctas), block, 0, st, p);
   if (rc != cudaSuccess || g.ctas == 1) return rc;
   // as many CTAs as run at once, of as many warps as there are parts to a unit
