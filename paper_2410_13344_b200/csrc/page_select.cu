@@ -8,6 +8,9 @@
 // The decisions are those of exact arithmetic, ties going to the lower page.  Scores are computed in fp32 together with a bound E of their error.
 // A page further than 2 E above or below the border between the last one taken and the first one left is decided by that; the few in
 // between are scored again in fp64.  (Summaries and queries of 16-bit elements: the products are exact in fp64 and their sums nearly always.)
+//
+// Two launches, 24 sequences of up to 32000 tokens (8 KV heads of 128, 117 MB of summaries): scores 22.6 us, 5.2 TB/s; selection 7.2.  One sequence of 131072: 9.2
+// and 8.2, of which the fp64 scores of the ten pages near the border are 2; both are rounds of memory latency one after another.
 #include <math.h>
 #include <string.h>
 

@@ -3,9 +3,15 @@
 //   out[b][h] = sum_s softmax_s(scale q[b][h] . k[s]) v[s],  lse = ln sum_s exp(scale q . k[s]),
 //   s over the slots [max(0, len - window), len), with a list over those of them that lie in its pages.
 //
-// Bound by HBM: every key and value once, for all query heads of its group.  A warp takes a page of 16 keys at a time, alone, from global
-// memory straight into the fragments of warp MMAs: no shared memory, no barriers until the end.  The sums run as one online softmax per warp;
-// the warps of a CTA meet in shared memory, the CTAs that a long cache is split over in a second kernel.
+// Bound by HBM: every key and value once, for all query heads of a unit (a KV head's group of them, or eight or sixteen of a larger one).  A warp takes a page of 16
+// keys at a time, alone, from global memory straight into the fragments of warp MMAs: no shared memory, no barriers until the end.  (Through a ring in shared memory, filled by
+// asynchronous copies: 64 sequences of up to 8192 tokens 221 us instead of 196, a selection of 24 x 128 pages 73 instead of 66; more instructions a page, and less L1 for the loads of
+// what runs next to it.)  The sums run as one online softmax per warp.  Who meets, in three forms:
+//   - a warp per unit, many short sequences: nobody;
+//   - a cluster per unit: the warps of a CTA in shared memory, its CTAs in each other's;
+//   - shares, long caches: all units' pages one after another in equal parts, one per CTA of a single wave; units that were cut are joined by a second kernel.
+// 64 sequences of up to 8192 tokens (64 heads on 8, heads of 128, 1257 MB) 190 us and 4 for the join: 6.6 TB/s in the main kernel, the measured copy rate; CTAs of equal shares
+// end between 172 and 190.  One sequence of 1000 tokens (32 heads on 8) 5.0 us: 2.0 to the first keys' arrival, 0.4 for their products, 1.8 for the meeting.
 #include <math.h>
 #include <string.h>
 
@@ -332,7 +338,8 @@ __device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c
     }
 }
 
-// fp32: plain FMA.  A lane owns DH / 32 elements of every key and value, a warp takes KEYS keys at a time for up to GH heads and has the next ones on their way.
+// fp32: plain FMA.  (Sixteen sequences of up to 8192 tokens, 8 heads on each of 8: 131 us, 4.7 TB/s; 1037 instructions for 8 keys of 8 heads, of which 512 multiply, at 2.1 a cycle with
+// the 8 warps that the registers leave an SM.  One head to a KV head: 123 MB in 20 us, 6.1 TB/s.)  A lane owns DH / 32 elements of every key and value, a warp takes KEYS keys at a time for up to GH heads and has the next ones on their way.
 // The lanes' KEYS x GH partial sums meet by halving, after which each lane has the scores of few keys to take the exponential of; the weights come back by
 // shuffles.
 template <int DH, int GH>
@@ -453,7 +460,6 @@ __device__ __forceinline__ void attend_f32(const PagedParams& p, const Piece& c,
 #pragma unroll
     for (int e = 0; e < E; ++e) sums.o[warp][h][lane * E + e] = o[h][e];
 }
-
 
 template <typename T, int DH, int HEADS, int AHEAD = 1>
 __device__ __forceinline__ void attend(const PagedParams& p, const Piece& c, Sums<DH, HEADS>& sums) {
@@ -714,9 +720,6 @@ constexpr int kWarpPages = 4;
 // Groups of more than eight heads in bf16: sixteen to a unit, which reads keys and values once for them; eight, and more CTAs, while those are no more pages than these in all.  (Heads of
 // 128, us with 16 / 8: 2 units of 256 pages 8.5 / 7.0, 32 of 64 14.0 / 8.4, 512 of 4 12.6 / 8.7; 32 of 256 19.9 / 17.0, ragged 11.9 / 15.6; 128 of 64 12.1 / 18.4; 512 of 256 102 / 167.)
 constexpr int kFewPages = 4096;
-// While two CTAs to an SM are enough (and a warp has more than one page), a cluster's warps have the registers for two pages ahead.  (64 units of 32 / 64 pages 8.0 / 10.3 -> 6.6 / 8.4 us, 128
-// of 32 / 64 10.5 / 16.7 -> 9.0 / 14.5.  In shares, and with fewer CTAs to have them so: no gain.)
-
 // Shares of fewer items cost more in joins than they save.  (1 unit of 64 pages, 4 / 8 / 16 items: 7.6 / 7.8 / 9.2 us; 64 of 24: 10.9 / 10.2 / 11.6.)
 constexpr int kMinShare = 8;
 // max_items: pages that a sequence can have to be looked at (a window may begin and end inside one)
@@ -746,6 +749,8 @@ int plan_paged(int dtype, int B, int H, int Hk, int head_dim, int max_len, int w
   if (g->together) {
     g->ctas = (int)g->units * g->together;
     g->joins = 0;
+    // while two CTAs to an SM are enough, and a warp has more than one page, the warps have the registers for two pages ahead (64 units of 32 / 64 pages 8.0 / 10.3 -> 6.6 / 8.4 us,
+    // 128 of 32 / 64 10.5 / 16.7 -> 9.0 / 14.5; in shares, and with fewer CTAs to have it so: no gain)
     g->deep = bf && g->ctas <= 2 * 148 && items > g->together * PA_WARPS * (128 / head_dim);
     return CERB_OK;
   }

@@ -316,6 +316,8 @@ __device__ __forceinline__ uint32_t upper(uint32_t a, uint32_t b, float) {
 // A run is what follows one another in the list within one page.  LANES threads own the runs of one head that begin in a window of `block` rows of the
 // list, each 16 bytes of the head: a run has one owner, so the page's minimum and maximum need no atomics and do not depend on any
 // order.  BATCH rows are in flight at once.  Keys and values are for different threads (blockIdx.y).
+// Bound by HBM: 16000 tokens of 8 heads of 128, bf16, 136 MB: 25 us, 5.4 TB/s.  64 tokens 1.8 us.  (More rows in flight, fewer CTAs to an SM: 28 us; copying and summaries by different
+// CTAs, the keys read a second time out of L2: 34; windows of fewer rows: 27 to 33.)
 template <typename T, int DH>
 __global__ void __launch_bounds__(256, 4) kv_append_kernel(const AppendParams p) {
   constexpr int LANES = DH * (int)sizeof(T) / 16, ROW = DH * (int)sizeof(T), BATCH = CERB_PAGE / 4;
