@@ -35,7 +35,7 @@ def _build_binding(force: bool) -> None:
                 os.path.join(cuda, "include")]
     _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
          + [x for i in includes for x in ("-isystem" if i != includes[0] else "-I", i)]
-         + [src, "-o", BINDING, "-L", lib, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-Wl,-rpath," + lib])
+         + [src, "-o", BINDING, "-L", lib, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda", "-Wl,-rpath," + lib])
 
 
 def _run(cmd) -> str:

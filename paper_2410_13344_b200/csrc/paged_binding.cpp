@@ -8,6 +8,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/core/LegacyTypeDispatch.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -104,15 +105,24 @@ void* operand(const at::Tensor& t, int64_t rows, int64_t heads, int64_t dh, cons
 }
 
 at::Tensor make(at::IntArrayRef sizes, at::ScalarType type, int device) {
-  return at::empty(sizes, at::TensorOptions().dtype(type).device(at::kCUDA, (c10::DeviceIndex)device));
+  return at::detail::empty_cuda(sizes, type, c10::Device(c10::kCUDA, (c10::DeviceIndex)device), std::nullopt);
 }
-// `n` elements of a tensor's memory, as a tensor of their own.
-at::Tensor part(const at::Tensor& t, int64_t at, int64_t n) {
-  auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(t.storage()), t.key_set(), t.dtype());
-  impl->set_storage_offset(at);
-  impl->set_sizes_contiguous({n});
-  return at::Tensor(std::move(impl));
-}
+// Results of a call are parts of one piece of memory, each on 16 bytes: an allocation is a microsecond.
+struct Parts {
+  at::Tensor all;
+  int64_t used = 0;
+  static int64_t bytes(at::IntArrayRef sizes, at::ScalarType type) {
+    return (c10::multiply_integers(sizes) * (int64_t)c10::elementSize(type) + 15) / 16 * 16;
+  }
+  Parts(int64_t bytes, int device) : all(make({bytes}, at::kByte, device)) {}
+  at::Tensor next(at::IntArrayRef sizes, at::ScalarType type) {
+    auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), c10::scalarTypeToTypeMeta(type));
+    impl->set_storage_offset(used / (int64_t)c10::elementSize(type));
+    impl->set_sizes_contiguous(sizes);
+    used += bytes(sizes, type);
+    return at::Tensor(std::move(impl));
+  }
+};
 void* stream_of(int device) { return (void*)c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream(); }
 
 // Runs a call with the tensors' device current, and turns what is thrown into a Python error.
@@ -163,16 +173,15 @@ PyObject* pages_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {       // n_n
     if (rows < 0) refuse(what, "rows is negative");
     if (s.B > 8192 || rows > 1 << 30) refuse(what, "more than 8192 requests or 2^30 rows", CERB_E_SHAPE);        // (ahead of the allocations)
     const c10::cuda::OptionalCUDAGuard on(c10::Device(c10::kCUDA, (c10::DeviceIndex)device));
-    // one piece of memory, each part on 16 bytes
     const int64_t sizes[5] = {rows, rows, rows, s.B + 1, s.B};
-    int64_t at[6] = {0};
-    for (int i = 0; i < 5; ++i) at[i + 1] = at[i] + (sizes[i] + 3) / 4 * 4;
-    const at::Tensor all = make({at[5]}, at::kInt, device);
+    int64_t bytes = 0;
+    for (const int64_t n : sizes) bytes += Parts::bytes({n}, at::kInt);
+    Parts parts(bytes, device);
     at::Tensor out[5];
     int32_t* p[5];
     for (int i = 0; i < 5; ++i) {
-      out[i] = part(all, at[i], sizes[i]);
-      p[i] = (int32_t*)all.data_ptr() + at[i];
+      out[i] = parts.next({sizes[i]}, at::kInt);
+      p[i] = (int32_t*)out[i].data_ptr();
     }
     done(lib.pages_plan(&s, want, rows, p[0], p[1], p[2], p[3], p[4], stream_of(device)), what);
     return PyObject_CallFunction(plan_class, "NNNNN", THPVariable_Wrap(out[0]), THPVariable_Wrap(out[1]), THPVariable_Wrap(out[2]), THPVariable_Wrap(out[3]),
@@ -294,7 +303,9 @@ PyObject* page_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor scratch = scratch_of(maybe(a[9], what), need, device, what);
     g.scratch = scratch.defined() ? scratch.data_ptr() : nullptr;
     g.scratch_bytes = scratch.defined() ? (size_t)scratch.numel() : 0;
-    const at::Tensor sel = make({g.B, g.n_kv_heads, g.max_sel}, at::kInt, device), n_sel = make({g.B}, at::kInt, device);
+    const int64_t lists[3] = {g.B, g.n_kv_heads, g.max_sel}, counts[1] = {g.B};
+    Parts parts(Parts::bytes(lists, at::kInt) + Parts::bytes(counts, at::kInt), device);
+    const at::Tensor sel = parts.next(lists, at::kInt), n_sel = parts.next(counts, at::kInt);
     g.sel = (int32_t*)sel.data_ptr();
     g.n_sel = (int32_t*)n_sel.data_ptr();
     done(lib.select(&g, stream_of(device)), what);
@@ -351,9 +362,11 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor scratch = scratch_of(maybe(a[11], what), need, device, what);
     g.scratch = scratch.defined() ? scratch.data_ptr() : nullptr;
     g.scratch_bytes = scratch.defined() ? (size_t)scratch.numel() : 0;
-    const at::Tensor out = make({g.B, g.n_heads, g.head_dim}, q.scalar_type(), device);
+    const int64_t outs[3] = {g.B, g.n_heads, g.head_dim};
+    Parts parts(Parts::bytes(outs, q.scalar_type()) + (lse_wanted ? Parts::bytes({g.B, g.n_heads}, at::kFloat) : 0), device);
+    const at::Tensor out = parts.next(outs, q.scalar_type());
     at::Tensor lse;
-    if (lse_wanted) lse = make({g.B, g.n_heads}, at::kFloat, device);
+    if (lse_wanted) lse = parts.next({g.B, g.n_heads}, at::kFloat);
     g.out = out.data_ptr();
     g.lse = lse_wanted ? (float*)lse.data_ptr() : nullptr;
     done(lib.attention(&g, stream_of(device)), what);
