@@ -31,6 +31,9 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 
 __device__ __forceinline__ int pages_of(int tokens) { return (int)(((unsigned)tokens + CERB_PAGE - 1) / CERB_PAGE); }
 
+// A slot of what a table or the stack names as a page.  (What can be no page, of a pool of less than 2^27 of them, gives a slot that nothing is written to.)
+__device__ __forceinline__ int slot_of(int page, int row) { return page >= 1 << 27 ? -1 : max(page, -(1 << 27)) * CERB_PAGE + row; }
+
 // Rows and pages, summed up together.
 struct Sums {
   long long rows;
@@ -151,7 +154,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_plan_kernel(const PagesParam
           pos = lens[b] + r - (b ? ends[b - 1] : 0);
           const int j = pos / CERB_PAGE, page = *source(b, j);
           if (pos % CERB_PAGE == 0) p.page_table[(size_t)b * p.max_pages + j] = page;      // (a page that begins here is new)
-          slot = page * CERB_PAGE + pos % CERB_PAGE;
+          slot = slot_of(page, pos % CERB_PAGE);
         }
       }
       p.slot[r] = slot;
@@ -181,7 +184,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_plan_kernel(const PagesParam
           for (int i = 0; i < 4; ++i) {
             pos[i] = at + i;
             seq[i] = b;
-            slot[i] = ((at + i) / CERB_PAGE == j ? page : page2) * CERB_PAGE + (at + i) % CERB_PAGE;
+            slot[i] = slot_of((at + i) / CERB_PAGE == j ? page : page2, (at + i) % CERB_PAGE);
           }
         }
       } else {
@@ -191,7 +194,7 @@ __global__ void __launch_bounds__(THREADS, 1) pages_plan_kernel(const PagesParam
           if (!give[b]) continue;
           const int at = lens[b] + r0 + i - (b ? ends[b - 1] : 0), page = *source(b, at / CERB_PAGE);
           if (at % CERB_PAGE == 0) p.page_table[(size_t)b * p.max_pages + at / CERB_PAGE] = page;
-          const int x = page * CERB_PAGE + at % CERB_PAGE;
+          const int x = slot_of(page, at % CERB_PAGE);
 #pragma unroll
           for (int k = 0; k < 4; ++k)
             if (k == i) { slot[k] = x; pos[k] = at; seq[k] = b; }
@@ -267,15 +270,15 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) pages_trim_kernel(const Pages
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       if (entry[i]) {
-        const int to = n_free + total - 1 - (w0 + 32 * i + (tid & 31));
-        if (to < p.free_cap) p.free_pages[to] = page[i];
+        const unsigned to = (unsigned)n_free + (unsigned)total - 1 - (unsigned)(w0 + 32 * i + (tid & 31));       // (less than 2^32)
+        if (to < (unsigned)p.free_cap) p.free_pages[to] = page[i];
         *entry[i] = -1;
       }
   }
   cluster_wait();
   if (cta != 0) return;
   for (int b = tid; b < p.B; b += PLAN_THREADS) p.len[b] = news[b];
-  if (tid == 0) *p.n_free = min(n_free + total, p.free_cap);
+  if (tid == 0) *p.n_free = (int)min((unsigned)n_free + (unsigned)total, (unsigned)p.free_cap);
 }
 
 // ---------------------------------------------------------------------------------------------

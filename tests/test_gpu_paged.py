@@ -107,6 +107,14 @@ def test_lengths_out_of_range_are_taken_to_the_nearest_in_range():
     assert n_free.tolist() == [3] and lens.tolist() == [0, 0, 0] and bool((table == -1).all())       # (room for one of the six)
 
 
+@pytest.mark.parametrize("rows", [40, 200000])                # a row to a lane, four rows to a lane
+def test_what_can_be_no_page_gives_no_slot(rows):
+    for page in (2 ** 27, 2 ** 28, 2 ** 31 - 1, -1, -(2 ** 28), -(2 ** 31)):
+        lens, table, free, n_free = i32([3]), i32([[page] + [-1] * 12499]), i32([page] * 12500), i32([12500])
+        plan = binding.pages_plan(i32([min(rows, 199990)]), lens, table, free, n_free, rows)
+        assert plan.granted.tolist() == [min(rows, 199990)] and bool((plan.slot < 0).all())
+
+
 # ---------------------------------------------------------------------------------------------- append
 
 
