@@ -391,7 +391,7 @@ int cerb_paged_attention(const cerb_paged_attn_args* args, void* stream);
 /* Picks the pages that a new token's queries may attend to most, per sequence and KV head.  A page's score is the largest, over the query heads of the KV head,
  * of sum_d max(q_d * k_min_d, q_d * k_max_d): no key of the page has a larger q . k.  The first n_first and the last n_last pages are always taken (n_first +
  * n_last <= max_sel), then the best scores, until max_sel are; all of a sequence of max_sel pages or fewer.  Decisions are made in
- * exact arithmetic, up to the rounding of sums of fp64; equal scores: the lower page; a score that is not a number is above all others.
+ * exact arithmetic, up to the rounding of sums of fp64; equal scores: the lower page; a score that is not a number counts as infinity.
  * sel: logical pages in ascending order, -1 behind the last one; n_sel[b] = min(pages of b, max_sel).
  * CERB_E_SHAPE: max_pages above 131072 (2 097 152 tokens), more than 64 query heads to a KV head, 2^16 KV heads or more, B * n_kv_heads of 2^23 or more. */
 typedef struct cerb_page_select_args {

@@ -68,15 +68,23 @@ __device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
   asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
+__device__ __forceinline__ float larger_size(float a, float b) {         // of |a| and |b|; a NaN if there is one
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)));
+  return r;
+}
 __device__ __forceinline__ uint32_t abs2(uint32_t a) { return a & 0x7fff7fffu; }
 
 // How far a score may be off, relative to S = sum_d |q_d| |k_d|, k_d the one of kmin_d and kmax_d that counts for q_d's sign.
 // bf16: q's positive and negative elements are products of their own, Dh / 16 <= 8 steps of the tensor cores each, and a step keeps at least 24 bits of the
 // largest of its 17 addends, each of which is at most the product's share of S: 8 x 17 x 2^-23 S, three more roundings and S's own error: under 2^-15.5 S.
-// fp32: chains of at most Dh / 32 + 5 roundings: under 2^-19 S.
+// fp32: chains of at most Dh / 32 + 5 roundings: under 2^-19 S.  Its S is taken with the larger of |kmin_d| and |kmax_d|, so that an infinity or a NaN in
+// either shows there.
+// A sum of so small numbers that its products or steps underflow is off by less than 2^-126 for each of them besides: kUnderflow.
 template <typename T> __device__ __forceinline__ float error_factor();
 template <> __device__ __forceinline__ float error_factor<bf16>() { return 2.1579186e-5f; }
 template <> __device__ __forceinline__ float error_factor<float>() { return 1.0f / 524288; }
+constexpr float kUnderflow = 2.4074124e-35f;                             // 2^-115, 2048 of them
 
 // Leaves what a warp's lanes know of a tile.
 __device__ __forceinline__ void leave_tile(TileScores* to, float bound, float lo, float hi, bool odd) {
@@ -222,7 +230,7 @@ __global__ void __launch_bounds__(SC_WARPS * 32, 3) page_score_bf16_kernel(const
         }
       }
     }
-    leave_tile(p.tile + (size_t)unit * p.tiles + now.tile, bound * error_factor<bf16>(), least, most, odd);
+    leave_tile(p.tile + (size_t)unit * p.tiles + now.tile, bound * error_factor<bf16>() + kUnderflow, least, most, odd);
     now = then;
     pages = pages_then;
     then = after;
@@ -273,7 +281,7 @@ __global__ void __launch_bounds__(SC_WARPS * 32, 4) page_score_f32_kernel(const 
           for (int e = 0; e < E; ++e) {
             const float k = x.x[e] >= 0.f ? hi[j].x[e] : lo[j].x[e];
             s[j] = fmaf(x.x[e], k, s[j]);
-            s[PAGES + j] = fmaf(fabsf(x.x[e]), fabsf(k), s[PAGES + j]);
+            s[PAGES + j] = fmaf(fabsf(x.x[e]), larger_size(hi[j].x[e], lo[j].x[e]), s[PAGES + j]);
           }
         }
         halve_sums(s, lane);
@@ -294,7 +302,7 @@ __global__ void __launch_bounds__(SC_WARPS * 32, 4) page_score_f32_kernel(const 
         }
       }
     }
-    leave_tile(p.tile + (size_t)unit * p.tiles + now.tile, bound * error_factor<float>(), least, most, odd);
+    leave_tile(p.tile + (size_t)unit * p.tiles + now.tile, bound * error_factor<float>() + kUnderflow, least, most, odd);
   }
 }
 

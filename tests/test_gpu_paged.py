@@ -411,6 +411,34 @@ def test_selection_from_caches_longer_than_was_said(dtype, hint):
     check_lists(sel, n_sel, ref.select(q, c.k_min, c.k_max, c.table, lens, 30), 30)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("N,K", [(40, 9), (700, 60), (3001, 130)])
+@pytest.mark.parametrize("power", [-72, -66, -60])
+def test_selection_where_products_underflow(dtype, N, K, power):
+    lo, hi = score_cache("plain", dtype, N)
+    lo, hi = lo * 2.0 ** power, hi * 2.0 ** power
+    table = torch.arange(N, dtype=torch.int32)[None]
+    q = torch.randn(1, 3, 64, generator=torch.Generator().manual_seed(2)).to(DT[dtype]) * 2.0 ** power
+    sel, n_sel = binding.page_select(q.cuda(), lo.cuda(), hi.cuda(), table.cuda(), i32([N * PAGE]), K, N * PAGE)
+    check_lists(sel, n_sel, ref.select(q, lo, hi, table, [N * PAGE], K), K)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("N,K", [(40, 9), (700, 60)])
+@pytest.mark.parametrize("bad,query", [(-math.inf, 0.0), (-math.inf, -0.0), (math.nan, 0.0), (math.nan, 1.0)])
+def test_selection_with_an_infinity_or_nan_on_the_side_that_does_not_count(dtype, N, K, bad, query):
+    lo, hi = score_cache("plain", dtype, N)
+    lo[7, :, 3] = bad
+    table = torch.arange(N, dtype=torch.int32)[None]
+    q = torch.randn(1, 3, 64, generator=torch.Generator().manual_seed(2)).to(DT[dtype])
+    q[0, :, 3] = q[0, :, 3].abs()
+    q[0, 1, 3] = query
+    want = ref.select(q, lo, hi, table, [N * PAGE], K)
+    assert 7 in want[0][0]
+    sel, n_sel = binding.page_select(q.cuda(), lo.cuda(), hi.cuda(), table.cuda(), i32([N * PAGE]), K, N * PAGE)
+    check_lists(sel, n_sel, want, K)
+
+
 def test_selection_with_queries_that_are_not_finite_and_pages_outside_the_pool():
     lo, hi = score_cache("plain", "bf16", 500)
     table = torch.arange(500, dtype=torch.int32)[None].repeat(2, 1)
