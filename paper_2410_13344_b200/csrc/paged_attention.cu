@@ -338,8 +338,8 @@ __device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c
     }
 }
 
-// fp32: plain FMA.  (Sixteen sequences of up to 8192 tokens, 8 heads on each of 8: 131 us, 4.7 TB/s; 1037 instructions for 8 keys of 8 heads, of which 512 multiply, at 2.1 a cycle with
-// the 8 warps that the registers leave an SM.  One head to a KV head: 123 MB in 20 us, 6.1 TB/s.)  A lane owns DH / 32 elements of every key and value, a warp takes KEYS keys at a time for up to GH heads and has the next ones on their way.
+// fp32, one or two heads to a unit, or four of 128: plain FMA.  (One head to a KV head: 123 MB in 20 us, 6.1 TB/s; 16 sequences of 8192 tokens, 4 heads on each of 8, 1074 MB: 164 us, 6.5 TB/s.)
+// A lane owns DH / 32 elements of every key and value, a warp takes KEYS keys at a time for up to GH heads and has the next ones on their way.
 // The lanes' KEYS x GH partial sums meet by halving, after which each lane has the scores of few keys to take the exponential of; the weights come back by
 // shuffles.
 template <int DH, int GH>
@@ -461,19 +461,212 @@ __device__ __forceinline__ void attend_f32(const PagedParams& p, const Piece& c,
     for (int e = 0; e < E; ++e) sums.o[warp][h][lane * E + e] = o[h][e];
 }
 
+// Pairs of fp32.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 twice(float x) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float2 parts_of(f32x2 a) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a));
+  return r;
+}
+
+// fp32, many heads to a unit: FMA on pairs.  A warp takes a page at a time and has the next one on its way.  What a lane reads of shared memory costs the SM 32 lanes' bytes
+// at 128 a cycle, the same address or not; so few bytes a lane decide the split.  Scores: lanes 8g .. 8g + 7 have keys g, g + 4, g + 8, g + 12, an eighth of the elements each (16 bytes of
+// every 128), the queries come out of shared memory, four chains of sums to a key and head keep the roundings in a row at Dh / 32 + 5.  Their GH x 4 sums meet by
+// halving, so that a lane has GH / 2 scores of one head.  Weights go through shared memory, two heads a pair; outputs: four columns to a lane
+// (heads of 64: every other key to each half of the warp).
+// 16 sequences of 8192 tokens, 8 heads of 128 on each of 8, 1074 MB: 170 us, 6.3 TB/s; 100 of 1600, 8 heads of 64, 655 MB: 120, 5.5 TB/s; the same with 16 heads, which takes two units: 185.
+// (With the lanes' way of the other fp32 form, 62 shuffles and 64 broadcasts for 8 keys of 8 heads: 216, 210, 326.  With a quarter of a key to a lane and weights twice in shared memory, the data
+// pipe of shared memory and L1 71 % busy: 191, 130, 201.  Four heads of 64 on each of 8, 16 x 9600 tokens: 127 -> 101 us, at the copy rate; four heads of 128: at the copy rate either way.)
+template <int DH, int GH>
+__device__ __forceinline__ void attend_f32_many(const PagedParams& p, const Piece& c, Sums<DH, GH>& sums) {
+  constexpr int CH = DH / 32, R = GH / 2, SIDES = 128 / DH, VK = CERB_PAGE / SIDES;
+  __shared__ alignas(16) float s_p[PA_WARPS][CERB_PAGE][GH], s_a[PA_WARPS][GH];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 3, t = lane & 7, side = lane / (DH / 4), col = lane % (DH / 4) * 4;
+  const int head = t * GH / 8, key0 = g + 4 * R * (t % (8 / GH));         // of the lane's scores
+  const size_t page_elems = (size_t)p.Hk * CERB_PAGE * DH;
+  const float* kp = reinterpret_cast<const float*>(p.k_pool) + (size_t)c.kvh * CERB_PAGE * DH + g * DH + 4 * t;
+  const float* vp = reinterpret_cast<const float*>(p.v_pool) + (size_t)c.kvh * CERB_PAGE * DH + side * DH + col;
+  f32x2 k[4][CH][2];
+  float4 v[VK];
+  auto load_k = [&](const PageRef& r) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int i = 0; i < CH; ++i)
+        asm volatile("ld.global.L1::no_allocate.L2::256B.v2.b64 {%0, %1}, [%2];"
+                     : "=l"(k[e][i][0]), "=l"(k[e][i][1]) : "l"(kp + r.at * page_elems + e * 4 * DH + 32 * i) : "memory");
+  };
+  auto load_v = [&](const PageRef& r) {
+#pragma unroll
+    for (int j = 0; j < VK; ++j)
+      asm volatile("ld.global.L1::no_allocate.L2::256B.v4.f32 {%0, %1, %2, %3}, [%4];"
+                   : "=f"(v[j].x), "=f"(v[j].y), "=f"(v[j].z), "=f"(v[j].w) : "l"(vp + r.at * page_elems + j * SIDES * DH) : "memory");
+  };
+  Walk walk(c);
+  auto next = [&]() {
+    for (;;) {
+      const PageRef r = walk.next(p, c);
+      if (r.at < 0 || (r.page * CERB_PAGE < c.sp.hi && (r.page + 1) * CERB_PAGE > c.sp.lo)) return r;
+    }
+  };
+  PageRef now = next();
+  if (now.at >= 0) { load_k(now); load_v(now); }
+  // the queries, where the outputs go at the end
+  float* s_q = &sums.o[warp][0][0];
+  for (int i = 4 * lane; i < GH * DH; i += 4 * 32) {
+    const int h = i / DH;
+    *reinterpret_cast<float4*>(s_q + i) =
+        h < c.heads ? *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.q) + (size_t)c.b * p.q_row + (size_t)(c.head0 + h) * p.q_head + i % DH)
+                    : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  __syncwarp();
+  f32x2 o[GH / 2][4];                                                    // [pair of heads][column]
+  float m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int h = 0; h < GH / 2; ++h)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[h][e] = 0;
+  while (now.at >= 0) {
+    const PageRef then = next();
+    float s[4 * GH];                                                     // [head][key]
+#pragma unroll
+    for (int h = 0; h < GH; ++h) {
+      f32x2 x[4][2];
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(s_q + h * DH + 32 * i + 4 * t);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[e][0] = i == 0 ? mul2(q.x, k[e][i][0]) : fma2(q.x, k[e][i][0], x[e][0]);
+          x[e][1] = i == 0 ? mul2(q.y, k[e][i][1]) : fma2(q.y, k[e][i][1], x[e][1]);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 y = parts_of(add2(x[e][0], x[e][1]));
+        s[4 * h + e] = y.x + y.y;
+      }
+    }
+    if (then.at >= 0) load_k(then);
+#pragma unroll
+    for (int w = 4, n = 2 * GH; w > 0; w >>= 1, n >>= 1)
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        const bool up = lane & w;
+        const float send = up ? s[i] : s[i + n], keep = up ? s[i + n] : s[i];
+        s[i] = keep + __shfl_xor_sync(0xffffffffu, send, w);
+      }
+    // s[i]: key key0 + 4 i
+    const int row0 = now.page * CERB_PAGE;
+    const bool ends = row0 < c.sp.lo || row0 + CERB_PAGE > c.sp.hi;
+    float mx = m;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      s[i] *= p.scale_log2;
+      const int row = row0 + key0 + 4 * i;
+      if (ends && (row < c.sp.lo || row >= c.sp.hi)) s[i] = -INFINITY;
+      mx = fmaxf(mx, s[i]);
+    }
+#pragma unroll
+    for (int w = 8; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+    if constexpr (GH == 4) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+    const float u = mx == -INFINITY ? 0.f : mx, a = exp2f(m - u);
+    const bool moved = __any_sync(0xffffffffu, a != 1.f);
+    m = mx;
+    l *= a;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const float x = exp2f(s[i] - u);
+      l += x;
+      s_p[warp][key0 + 4 * i][head] = x;
+    }
+    if (moved && key0 == 0) s_a[warp][head] = a;
+    if (ends) {
+#pragma unroll
+      for (int j = 0; j < VK; ++j) {
+        const int row = row0 + j * SIDES + side;
+        if (row < c.sp.lo || row >= c.sp.hi) v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+    }
+    __syncwarp();
+    if (moved) {
+#pragma unroll
+      for (int h = 0; h < GH / 2; ++h) {
+        const f32x2 x = *reinterpret_cast<const f32x2*>(&s_a[warp][2 * h]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[h][e] = mul2(o[h][e], x);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < VK; ++j) {
+      const f32x2 x[4] = {twice(v[j].x), twice(v[j].y), twice(v[j].z), twice(v[j].w)};
+#pragma unroll
+      for (int h = 0; h < GH / 2; h += 2) {
+        const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(&s_p[warp][j * SIDES + side][2 * h]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          o[h][e] = fma2(w.x, x[e], o[h][e]);
+          o[h + 1][e] = fma2(w.y, x[e], o[h + 1][e]);
+        }
+      }
+    }
+    if (then.at >= 0) load_v(then);
+    __syncwarp();
+    now = then;
+  }
+#pragma unroll
+  for (int w = 8; w < 32; w <<= 1) l += __shfl_xor_sync(0xffffffffu, l, w);
+  if constexpr (GH == 4) l += __shfl_xor_sync(0xffffffffu, l, 1);
+  if (key0 == 0) { sums.m[warp][head] = m; sums.l[warp][head] = l; }
+#pragma unroll
+  for (int h = 0; h < GH / 2; ++h) {
+    float2 x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (SIDES == 2) o[h][e] = add2(o[h][e], __shfl_xor_sync(0xffffffffu, o[h][e], 16));
+      x[e] = parts_of(o[h][e]);
+    }
+    if (side) continue;
+    *reinterpret_cast<float4*>(&sums.o[warp][2 * h][col]) = make_float4(x[0].x, x[1].x, x[2].x, x[3].x);
+    *reinterpret_cast<float4*>(&sums.o[warp][2 * h + 1][col]) = make_float4(x[0].y, x[1].y, x[2].y, x[3].y);
+  }
+}
+
 template <typename T, int DH, int HEADS, int AHEAD = 1>
 __device__ __forceinline__ void attend(const PagedParams& p, const Piece& c, Sums<DH, HEADS>& sums) {
   if constexpr (sizeof(T) == 2) attend_bf16<DH, HEADS / 8, AHEAD>(p, c, sums);
+  else if constexpr (HEADS == 8 || (HEADS == 4 && DH == 64)) attend_f32_many<DH, HEADS>(p, c, sums);
   else attend_f32<DH, HEADS>(p, c, sums);
 }
 
 // CTAs that fit an SM, as the kernels' registers allow.
-template <typename T, int HEADS>
-constexpr int ctas_per_sm() { return sizeof(T) == 2 ? (HEADS == 8 ? 3 : 2) : HEADS <= 2 ? 4 : HEADS == 4 ? 3 : 2; }
+// (fp32, 8 heads of 64, 2 / 3 / 4: 100 sequences of 100 pages 126 / 120 / 154 us.)
+template <typename T, int DH, int HEADS>
+constexpr int ctas_per_sm() { return sizeof(T) == 2 ? (HEADS == 8 ? 3 : 2) : HEADS <= 2 ? 4 : HEADS == 4 || DH == 64 ? 3 : 2; }
 
 // Every CTA a share.
 template <typename T, int DH, int HEADS>
-__global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_attn_kernel(const PagedParams p) {
+__global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, DH, HEADS>()) paged_attn_kernel(const PagedParams p) {
   __shared__ Sums<DH, HEADS> sums;
   griddep_wait();
   griddep_launch();
@@ -542,7 +735,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_
 
 // Every unit a cluster, which meets in its CTAs' shared memory: each CTA joins a part of the outputs, sent to it by all.
 template <typename T, int DH, int HEADS, int AHEAD>
-__global__ void __launch_bounds__(PA_WARPS * 32, AHEAD == 1 ? ctas_per_sm<T, HEADS>() : 2) paged_attn_cluster_kernel(const PagedParams p) {
+__global__ void __launch_bounds__(PA_WARPS * 32, AHEAD == 1 ? ctas_per_sm<T, DH, HEADS>() : 2) paged_attn_cluster_kernel(const PagedParams p) {
   __shared__ Sums<DH, HEADS> sums;
   __shared__ alignas(16) float s_o[HEADS * DH];                          // [CTA][its part of the outputs]
   __shared__ alignas(16) float2 s_ml[HEADS][PA_CLUSTER];
@@ -608,7 +801,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32, AHEAD == 1 ? ctas_per_sm<T, HEA
 
 // Every unit a warp, for many short sequences: nothing to meet, no barrier.
 template <typename T, int DH, int HEADS>
-__global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, HEADS>()) paged_attn_warp_kernel(const PagedParams p) {
+__global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, DH, HEADS>()) paged_attn_warp_kernel(const PagedParams p) {
   __shared__ Sums<DH, HEADS> sums;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long unit = (long long)blockIdx.x * PA_WARPS + warp;
@@ -711,7 +904,8 @@ struct PagedPlan {
 // shares and a join beyond that.  (bf16, 4 x 8 heads of 128, all sequences alike / between half as long and as long, every fourth idle; us with
 // clusters, with shares: 64 units of 8 pages 5.8 / 5.8, 7.0 / 13.0; 8 of 400 11.4 / 9.6, 13.4 / 15.2; 192 of 64 19.7 / 17.9, 23.3 / 19.5; 1 of 400 8.4, 9.8.  More than
 // that to a warp, the longest decide: 256 units of 64 29.6 / 27.9, 28.2 / 21.8; 128 of 160 35.8 / 32.2, 36.4 / 24.3; 1 of 1000 14.1, 10.6.  And of more than one wave: 512 units
-// of 32 35.9 / 22.8, 30.3 / 23.8; 2048 of 24 82 / 56, 73 / 52.  fp32 from four heads of a unit on: half as many, 32 units of 300 pages 37 / 31, 34 / 23.)
+// of 32 35.9 / 22.8, 30.3 / 23.8; 2048 of 24 82 / 56, 73 / 52.  fp32 with eight heads to a unit, or four of 128: half as many, 32 units of 300 pages, 8 heads of 128, 34.4 / 29.7, 36.2 / 25.2;
+// four heads of 64: 128 units of 60 13.7 / 12.1, 16.4 / 14.2; 400 of 40 23.8 / 15.6, 28.5 / 18.2.)
 constexpr int kClusterPages = 12;
 // Many short sequences: a warp per unit, while that is no more pages than these (four times as many where the units are more than one wave of CTAs).  (Pages of a sequence, all
 // alike, us with a CTA / a warp per unit: 384 units of 1 / 4 / 8 pages 6.6 / 7.7 / 9.0, 4.8 / 7.1 / 9.6; 1024 of 1 / 8 / 16 18.7 / 27.0 / 36.5, 6.8 / 17.3 / 28.8; 5120 of 1 / 8
@@ -734,11 +928,12 @@ int plan_paged(int dtype, int B, int H, int Hk, int head_dim, int max_len, int w
   g->units_h = (G + g->heads_unit - 1) / g->heads_unit;
   g->units = (long long)B * Hk * g->units_h;
   if (g->units * std::max(g->heads_unit, PA_CLUSTER) > 0x7fffffffll) return CERB_E_SHAPE;
-  const int at_once = 148 * (bf ? (g->heads_unit == 8 ? ctas_per_sm<bf16, 8>() : ctas_per_sm<bf16, 16>())
-                                : g->heads_unit == 8 ? ctas_per_sm<float, 8>() : g->heads_unit == 4 ? ctas_per_sm<float, 4>() : ctas_per_sm<float, 2>());
+  const int at_once = 148 * (bf ? (g->heads_unit == 8 ? ctas_per_sm<bf16, 64, 8>() : ctas_per_sm<bf16, 64, 16>())
+                                : g->heads_unit == 8 ? (head_dim == 64 ? ctas_per_sm<float, 64, 8>() : ctas_per_sm<float, 128, 8>())
+                                : g->heads_unit == 4 ? ctas_per_sm<float, 64, 4>() : ctas_per_sm<float, 64, 2>());
   g->together = 1;
   while (g->together < PA_CLUSTER && g->units * g->together * 2 <= at_once && g->together * 2 * PA_WARPS <= items + PA_WARPS) g->together *= 2;
-  if (g->units > at_once || items > (long long)g->together * PA_WARPS * (bf || g->heads_unit <= 2 ? kClusterPages : kClusterPages / 2)) g->together = 0;
+  if (g->units > at_once || items > (long long)g->together * PA_WARPS * (bf || g->heads_unit <= 2 || g->heads_unit * head_dim == 256 ? kClusterPages : kClusterPages / 2)) g->together = 0;
   g->min_share = kMinShare;
   if (g->units > at_once ? items <= 4 * kWarpPages : g->units * 2 > at_once && items <= kWarpPages) g->together = -1;
   if (g->together < 0) {

@@ -299,6 +299,20 @@ def test_attention_over_listed_pages(dtype, window):
     check(out, lse, ref.attention(q, c.k_pool, c.v_pool, c.table, lens, 0.2, window, used))
 
 
+@pytest.mark.parametrize("G,D", [(3, 64), (4, 64), (5, 128), (8, 128), (8, 64), (11, 64), (16, 128)])
+@pytest.mark.parametrize("lens,window", [([1], 0), ([24, 3, 0, 200] * 60, 0), ([9000, 0, 7000], 0), ([700, 1, 555], 99)])
+def test_fp32_attention_of_many_heads_in_every_form(G, D, lens, window):
+    c = Cache(lens, 2, D, "fp32", G)
+    q, gq = c.queries(2 * G, D)
+    out, lse = binding.paged_attention(gq, *c.gpu, c.glens, 0.1, max(lens), window=window)
+    check(out, lse, ref.attention(q, c.k_pool, c.v_pool, c.table, lens, 0.1, window))
+    # a list in descending order, its first page twice
+    K = 30
+    lists = [[[ref.pages_of(n) - 1 - max(i - 1, 0) for i in range(K)] for _ in range(2)] for n in lens]
+    out, lse = binding.paged_attention(gq, *c.gpu, c.glens, 0.1, max(lens), window=window, sel=i32(lists), n_sel=i32([K] * len(lens)))
+    check(out, lse, ref.attention(q, c.k_pool, c.v_pool, c.table, lens, 0.1, window, lists))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_pages_outside_the_pool_hold_no_keys(dtype):
     lens = [200, 40, 16]
