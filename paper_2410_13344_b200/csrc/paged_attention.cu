@@ -461,34 +461,6 @@ __device__ __forceinline__ void attend_f32(const PagedParams& p, const Piece& c,
     for (int e = 0; e < E; ++e) sums.o[warp][h][lane * E + e] = o[h][e];
 }
 
-// Pairs of fp32.
-typedef unsigned long long f32x2;
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
-  f32x2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-  f32x2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
-  f32x2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ f32x2 twice(float x) {
-  f32x2 r;
-  asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(x));
-  return r;
-}
-__device__ __forceinline__ float2 parts_of(f32x2 a) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a));
-  return r;
-}
-
 // fp32, many heads to a unit: FMA on pairs.  A warp takes a page at a time and has the next one on its way.  What a lane reads of shared memory costs the SM 32 lanes' bytes
 // at 128 a cycle, the same address or not; so few bytes a lane decide the split.  Scores: lanes 8g .. 8g + 7 have keys g, g + 4, g + 8, g + 12, an eighth of the elements each (16 bytes of
 // every 128), the queries come out of shared memory, four chains of sums to a key and head keep the roundings in a row at Dh / 32 + 5.  Their GH x 4 sums meet by
@@ -671,7 +643,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, DH, HEADS>()) pa
   griddep_wait();
   griddep_launch();
   const long long uh = (long long)p.Hk * p.units_h;
-  const Share sh = share_of(p.B, [&](int b) { return span_of(p, b).items * uh; }, blockIdx.x, gridDim.x, p.min_share);
+  const Share sh = share_of(p.B, [&](int b) { return span_of(p, b).items * uh; }, blockIdx.x, gridDim.x, p.min_share, p.B * uh);
   // sequences without anything to look at
   for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
     if (span_of(p, b).items) continue;
@@ -915,13 +887,14 @@ constexpr int kWarpPages = 4;
 // 128, us with 16 / 8: 2 units of 256 pages 8.5 / 7.0, 32 of 64 14.0 / 8.4, 512 of 4 12.6 / 8.7; 32 of 256 19.9 / 17.0, ragged 11.9 / 15.6; 128 of 64 12.1 / 18.4; 512 of 256 102 / 167.)
 constexpr int kFewPages = 4096;
 // Shares of fewer items cost more in joins than they save.  (1 unit of 64 pages, 4 / 8 / 16 items: 7.6 / 7.8 / 9.2 us; 64 of 24: 10.9 / 10.2 / 11.6.)
+// Of units that have fewer in the mean, a share takes one: else up to eight stand one behind another.  (512 units of a page, at most 512 by the caller's word, 20.9 -> 7.5 us.)
 constexpr int kMinShare = 8;
 // max_items: pages that a sequence can have to be looked at (a window may begin and end inside one)
 int plan_paged(int dtype, int B, int H, int Hk, int head_dim, int max_len, int window, int max_sel, PagedPlan* g) {
   if (dtype != CERB_F32 && dtype != CERB_BF16) return CERB_E_ARG;
   if (B < 0 || H < 1 || Hk < 1 || H % Hk || (head_dim != 64 && head_dim != 128)) return CERB_E_SHAPE;
   const long long whole = ((long long)max_len + CERB_PAGE - 1) / CERB_PAGE, in_window = ((long long)window + 2 * CERB_PAGE - 2) / CERB_PAGE;
-  const long long items = max_sel > 0 ? max_sel : window > 0 && in_window < whole ? in_window : whole;
+  const long long items = max_sel > 0 ? std::min((long long)max_sel, whole) : window > 0 && in_window < whole ? in_window : whole;
   const int G = H / Hk;
   const bool bf = dtype == CERB_BF16;
   g->heads_unit = bf ? (G > 8 && (long long)B * Hk * ((G + 7) / 8) * items > kFewPages ? 16 : 8) : G > 4 ? 8 : G > 2 ? 4 : G;

@@ -12,6 +12,35 @@ __device__ __forceinline__ uint4 ld16(const void* src) {
   return r;
 }
 
+// Pairs of fp32.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 pair_of(float x, float y) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ f32x2 twice(float x) { return pair_of(x, x); }
+__device__ __forceinline__ float2 parts_of(f32x2 a) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a));
+  return r;
+}
+
 // Sums over a warp's lanes of N values each, by halving: every exchange carries half of what is left, as many shuffles as values.  Afterwards lane i has
 // in x[0 .. R-1], R = N / 32, the sums of the values i R .., with N < 32 in x[0] that of the value i / (32 / N).
 template <int N>
@@ -40,10 +69,11 @@ struct Share {
   int b;                        // the sequence that begin lies in,
   long long off;                // and where in it
 };
-// Share `index` of `shares`, each of min_share items at least.  By a warp, which sums the items up for itself: a few hundred sequences
+// Share `index` of `shares`, each of min_share items at least, or of what one of the `units` has in the mean where that is less: short units are not put one behind
+// another while there are CTAs for them.  By a warp, which sums the items up for itself: a few hundred sequences
 // are a few loads to a lane, and no barrier.
 template <typename F>
-__device__ __forceinline__ Share share_of(int B, F items, int index, int shares, int min_share) {
+__device__ __forceinline__ Share share_of(int B, F items, int index, int shares, int min_share, long long units) {
   const int lane = threadIdx.x & 31, per = (B + 31) / 32, b0 = min(B, lane * per), b1 = min(B, b0 + per);
   long long mine = 0;
 #pragma unroll 4
@@ -57,7 +87,7 @@ __device__ __forceinline__ Share share_of(int B, F items, int index, int shares,
   const long long total = __shfl_sync(0xffffffffu, sum, 31);
   Share s;
   const long long even = total >> 32 ? (total + shares - 1) / shares : ((unsigned)total + (unsigned)(shares - 1)) / (unsigned)shares;
-  s.size = max(even, (long long)min_share);
+  s.size = max(even, total >= min_share * units ? (long long)min_share : (long long)max(1u, (unsigned)total / (unsigned)units));
   s.begin = min(total, s.size * index);
   s.end = min(total, s.begin + s.size);
   const bool here = s.begin >= sum - mine && s.begin < sum;
