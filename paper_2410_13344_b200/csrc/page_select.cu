@@ -141,7 +141,6 @@ __global__ void __launch_bounds__(SC_WARPS * 32, 3) page_score_bf16_kernel(const
   constexpr int KC = DH / 32;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   griddep_wait();
-  griddep_launch();
   TileWalk now = walk_tiles(p);
   struct Pages {
     int at[2];
@@ -256,7 +255,6 @@ __global__ void __launch_bounds__(SC_WARPS * 32, 4) page_score_f32_kernel(const 
   };
   const int lane = threadIdx.x & 31;
   griddep_wait();
-  griddep_launch();
   float most_q[E];                                                       // of the heads of `have`
   int have = -1;
   for (TileWalk now = walk_tiles(p); now.left > 0; next_tile(p, now)) {

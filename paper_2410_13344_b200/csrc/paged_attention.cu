@@ -631,6 +631,11 @@ __device__ __forceinline__ void attend(const PagedParams& p, const Piece& c, Sum
   else attend_f32<DH, HEADS>(p, c, sums);
 }
 
+// The next kernel may be scheduled while this one runs only where that leaves it room on every SM: its waiting CTAs otherwise take the places of those that end first, and
+// run on crowded SMs while others idle.  (us a pass with / without: 64 sequences of up to 8192 tokens 192 / 189.7, window of 16001 40.4 / 38.8, 123 MB of fp32 in clusters 23.2 / 21.7;
+// 128 CTAs for one sequence of 1000 tokens 5.4 / 5.5.)
+constexpr int kEarlyCtas = 148;
+
 // CTAs that fit an SM, as the kernels' registers allow.
 // (fp32, 8 heads of 64, 2 / 3 / 4: 100 sequences of 100 pages 126 / 120 / 154 us.)
 template <typename T, int DH, int HEADS>
@@ -641,7 +646,6 @@ template <typename T, int DH, int HEADS>
 __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, DH, HEADS>()) paged_attn_kernel(const PagedParams p) {
   __shared__ Sums<DH, HEADS> sums;
   griddep_wait();
-  griddep_launch();
   const long long uh = (long long)p.Hk * p.units_h;
   const Share sh = share_of(p.B, [&](int b) { return span_of(p, b).items * uh; }, blockIdx.x, gridDim.x, p.min_share, p.B * uh);
   // sequences without anything to look at
@@ -721,7 +725,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32, AHEAD == 1 ? ctas_per_sm<T, DH,
   c.head0 = c.kvh * p.G + part * HEADS;
   c.heads = min(HEADS, p.G - part * HEADS);
   griddep_wait();
-  griddep_launch();
+  if (gridDim.x <= kEarlyCtas) griddep_launch();
   // (the items are dealt out one by one, so that the first ones can be looked up before the length is known)
   c.item0 = rank * PA_WARPS;
   c.stride = n * PA_WARPS;
@@ -778,7 +782,6 @@ __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, DH, HEADS>()) pa
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long unit = (long long)blockIdx.x * PA_WARPS + warp;
   griddep_wait();
-  griddep_launch();
   const int part = (int)(unit % p.units_h);
   Piece c;
   c.kvh = (int)(unit / p.units_h % p.Hk);
