@@ -631,11 +631,9 @@ __device__ __forceinline__ void attend(const PagedParams& p, const Piece& c, Sum
   else attend_f32<DH, HEADS>(p, c, sums);
 }
 
-// The next kernel may be scheduled while this one runs only where that leaves it room on every SM: its waiting CTAs otherwise take the places of those that end first, and
-// run on crowded SMs while others idle.  (us a pass with / without: 64 sequences of up to 8192 tokens 192 / 189.7, window of 16001 40.4 / 38.8, 123 MB of fp32 in clusters 23.2 / 21.7;
-// 128 CTAs for one sequence of 1000 tokens 5.4 / 5.5.)
-constexpr int kEarlyCtas = 148;
-
+// None of the three forms lets the next kernel be scheduled before it ends: waiting CTAs take the places of those that end first, and then run on crowded SMs while others idle.
+// (us a pass that follows another, with an early release / without: 64 sequences of up to 8192 tokens 192 / 189.7, a window of 16001 40.4 / 38.8, 123 MB of fp32 in clusters 23.2 / 21.7, 32 units
+// of 60 pages 7.3 / 6.5, 1024 of 16 27.8 / 24.6; one sequence of 1000 tokens 5.4 / 5.5.)
 // CTAs that fit an SM, as the kernels' registers allow.
 // (fp32, 8 heads of 64, 2 / 3 / 4: 100 sequences of 100 pages 126 / 120 / 154 us.)
 template <typename T, int DH, int HEADS>
@@ -725,7 +723,6 @@ __global__ void __launch_bounds__(PA_WARPS * 32, AHEAD == 1 ? ctas_per_sm<T, DH,
   c.head0 = c.kvh * p.G + part * HEADS;
   c.heads = min(HEADS, p.G - part * HEADS);
   griddep_wait();
-  if (gridDim.x <= kEarlyCtas) griddep_launch();
   // (the items are dealt out one by one, so that the first ones can be looked up before the length is known)
   c.item0 = rank * PA_WARPS;
   c.stride = n * PA_WARPS;
