@@ -33,8 +33,8 @@ constexpr int kMaxSelectPages = 1 << 17;    // (a bit mask of them lies in share
 // What is known of the scores of a tile of pages (of those of it that are up for selection).
 struct TileScores {
   float bound;                 // of the error of its scores
-  float lo, hi;                // smallest and largest score
-  int odd;                     // scores that are not finite
+  float lo, hi;                // smallest and largest score of those that lie in the pool
+  int rest;                    // bit 0: scores among them that are not finite; above it the number of pages that lie nowhere
 };
 constexpr int kTile = 16;      // pages
 
@@ -92,7 +92,7 @@ template <> __device__ __forceinline__ float error_factor<float>() { return 1.0f
 constexpr float kUnderflow = 2.4074124e-35f;                             // 2^-115, 2048 of them
 
 // Leaves what a warp's lanes know of a tile.
-__device__ __forceinline__ void leave_tile(TileScores* to, float bound, float lo, float hi, bool odd) {
+__device__ __forceinline__ void leave_tile(TileScores* to, float bound, float lo, float hi, bool odd, int nowhere) {
 #pragma unroll
   for (int w = 1; w < 32; w <<= 1) {
     bound = fmaxf(bound, __shfl_xor_sync(0xffffffffu, bound, w));
@@ -100,7 +100,8 @@ __device__ __forceinline__ void leave_tile(TileScores* to, float bound, float lo
     hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, w));
   }
   odd = __any_sync(0xffffffffu, odd);
-  if ((threadIdx.x & 31) == 0) *reinterpret_cast<float4*>(to) = make_float4(bound, lo, hi, __int_as_float(odd));
+  nowhere = __reduce_add_sync(0xffffffffu, nowhere);
+  if ((threadIdx.x & 31) == 0) *reinterpret_cast<float4*>(to) = make_float4(bound, lo, hi, __int_as_float(2 * nowhere + odd));
 }
 
 // A warp's way through its share of the tiles of all units whose pages have to be selected from.
@@ -215,6 +216,7 @@ __global__ void __launch_bounds__(SC_WARPS * 32, 3) page_score_bf16_kernel(const
     }
     float least = INFINITY, most = -INFINITY;
     bool odd = false;
+    int nowhere = 0;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       float s = nan[e] ? NAN : best[e];
@@ -228,13 +230,17 @@ __global__ void __launch_bounds__(SC_WARPS * 32, 3) page_score_bf16_kernel(const
       if (page < now.N) {
         if (t == 0) p.score[(size_t)unit * p.max_pages + page] = s;
         if (page >= p.n_first && page < now.N - p.n_last) {
-          odd |= !(fabsf(s) < INFINITY);
-          least = fminf(least, s);
-          most = fmaxf(most, s);
+          if (pages.at[e] < 0) {
+            nowhere += t == 0;
+          } else {
+            odd |= !(fabsf(s) < INFINITY);
+            least = fminf(least, s);
+            most = fmaxf(most, s);
+          }
         }
       }
     }
-    leave_tile(p.tile + (size_t)unit * p.tiles + now.tile, bound * error_factor<bf16>() + kUnderflow, least, most, odd);
+    leave_tile(p.tile + (size_t)unit * p.tiles + now.tile, bound * error_factor<bf16>() + kUnderflow, least, most, odd, nowhere);
     now = then;
     pages = pages_then;
     then = after;
@@ -276,6 +282,7 @@ __global__ void __launch_bounds__(SC_WARPS * 32, 4) page_score_f32_kernel(const 
     }
     float bound = 0.f, least = INFINITY, most = -INFINITY;
     bool odd = false;
+    int nowhere = 0;
 #pragma unroll 1
     for (int half = 0; half < kTile / PAGES; ++half) {
       Pairs hi[PAGES], lo[PAGES];
@@ -335,13 +342,17 @@ __global__ void __launch_bounds__(SC_WARPS * 32, 4) page_score_f32_kernel(const 
         const float x = at < 0 ? -INFINITY : nan ? NAN : best;
         if (lane % 4 == 0) p.score[(size_t)unit * p.max_pages + page] = x;
         if (page >= p.n_first && page < now.N - p.n_last) {
-          odd |= !(fabsf(x) < INFINITY);
-          least = fminf(least, x);
-          most = fmaxf(most, x);
+          if (at < 0) {
+            nowhere += lane % 4 == 0;
+          } else {
+            odd |= !(fabsf(x) < INFINITY);
+            least = fminf(least, x);
+            most = fmaxf(most, x);
+          }
         }
       }
     }
-    leave_tile(p.tile + (size_t)unit * p.tiles + now.tile, bound * error_factor<float>() + kUnderflow, least, most, odd);
+    leave_tile(p.tile + (size_t)unit * p.tiles + now.tile, bound * error_factor<float>() + kUnderflow, least, most, odd, nowhere);
   }
 }
 
@@ -444,7 +455,7 @@ __global__ void __launch_bounds__(SEL_THREADS, 1024 / SEL_THREADS) page_select_k
   __shared__ int red[32], hist[SEL_BINS];
   __shared__ int list[SEL_LIST], list_at[SEL_LIST];
   __shared__ unsigned long long again[SEL_LIST];
-  __shared__ int s_lo, s_hi, s_n, s_bin, s_above, s_bound, s_odd;
+  __shared__ int s_lo, s_hi, s_n, s_bin, s_above, s_bound, s_odd, s_nowhere;
   extern __shared__ unsigned taken[];                                    // a bit for each page of the table's row, then the scores that are kept
   float* kept = reinterpret_cast<float*>(taken + (p.max_pages + 31) / 32);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -452,7 +463,7 @@ __global__ void __launch_bounds__(SEL_THREADS, 1024 / SEL_THREADS) page_select_k
   if (tid == 0) {
     s_lo = ordered(INFINITY);
     s_hi = ordered(-INFINITY);
-    s_n = s_bound = s_odd = 0;
+    s_n = s_bound = s_odd = s_nowhere = 0;
   }
   hist[tid] = 0;
   griddep_wait();
@@ -500,19 +511,23 @@ __global__ void __launch_bounds__(SEL_THREADS, 1024 / SEL_THREADS) page_select_k
   if (p.scored) {
     const int tiles = (N + kTile - 1) / kTile;
     if (tid >= tiles) known = make_float4(0.f, INFINITY, -INFINITY, 0.f);
-    bool odd = __float_as_int(known.w) != 0;
+    bool odd = __float_as_int(known.w) & 1;
+    int nowhere = __float_as_int(known.w) >> 1;
     for (int i = tid + SEL_THREADS; i < tiles; i += SEL_THREADS) {
       const float4 k = of_tile[i];
       known.x = fmaxf(known.x, k.x);
       known.y = fminf(known.y, k.y);
       known.z = fmaxf(known.z, k.z);
-      odd |= __float_as_int(k.w) != 0;
+      odd |= __float_as_int(k.w) & 1;
+      nowhere += __float_as_int(k.w) >> 1;
     }
     if (tid / 32 * 32 < tiles) {
       const int lw = __reduce_min_sync(0xffffffffu, ordered(known.y)), hw = __reduce_max_sync(0xffffffffu, ordered(known.z));
       const int e = __reduce_max_sync(0xffffffffu, __float_as_int(known.x));   // (not negative, not a NaN)
       odd = __any_sync(0xffffffffu, odd);
+      nowhere = __reduce_add_sync(0xffffffffu, nowhere);
       if (lane == 0) {
+        if (nowhere) atomicAdd(&s_nowhere, nowhere);
         atomicMin(&s_lo, lw);
         atomicMax(&s_hi, hw);
         atomicMax(&s_bound, e);
@@ -527,7 +542,9 @@ __global__ void __launch_bounds__(SEL_THREADS, 1024 / SEL_THREADS) page_select_k
   const bool all_again = !p.scored || s_odd || !(E < INFINITY);          // scores that are not finite decide nothing
   int above = 0;                                                         // pages above hi
   float t_lo = -INFINITY, t_hi = INFINITY;
-  if (!all_again && want > 0) {
+  if (!all_again && last - first - s_nowhere <= want) {
+    t_hi = -INFINITY;                                                    // all pages that lie in the pool, and the first ones of the others
+  } else if (!all_again && want > 0) {
 #pragma unroll 1
     for (int level = 0; level < 8; ++level) {
       const float inv = (float)SEL_BINS / (hi - lo);

@@ -426,6 +426,26 @@ def test_selection_from_caches_longer_than_was_said(dtype, hint):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("gone", ["one", "half", "all but few", "all but as many", "all", "all but few alike", "all but first and last"])
+@pytest.mark.parametrize("N,K", [(60, 9), (700, 60), (2500, 130), (9000, 300)])
+def test_selection_from_tables_with_pages_that_are_gone(dtype, gone, N, K):
+    lo, hi = score_cache("equal" if gone == "all but few alike" else "plain", dtype, N)
+    table = torch.tensor([random.Random(N).sample(range(N), N)], dtype=torch.int32)
+    stay = {"one": N - 1, "half": N // 2, "all but few": K // 2, "all but as many": K, "all": 0, "all but few alike": K // 2, "all but first and last": 2}[gone]
+    away = random.Random(K).sample(range(1, N - 1), N - 2)[:N - stay] if stay else list(range(N))
+    table[0, away] = torch.tensor([[-1, N, 2 ** 31 - 1, -2 ** 31][i % 4] for i in range(len(away))], dtype=torch.int32)
+    q = torch.randn(1, 3, 64, generator=torch.Generator().manual_seed(1)).to(DT[dtype])
+    sel, n_sel = binding.page_select(q.cuda(), lo.cuda(), hi.cuda(), table.cuda(), i32([N * PAGE]), K, N * PAGE)
+    at, rows = table[0].long(), ref.pages_of(N * PAGE)
+    live = (at >= 0) & (at < N)
+    x, a, b = q[0].double(), lo[at.clamp(0, N - 1), 0].double(), hi[at.clamp(0, N - 1), 0].double()
+    score = torch.where(live, (x.clamp(min=0) @ b.T + x.clamp(max=0) @ a.T).amax(0), -math.inf)
+    score[0] = score[-1] = math.inf
+    want = torch.sort(torch.sort(score, descending=True, stable=True).indices[:K]).values
+    assert rows == N and sel[0, 0].tolist() == want.tolist() and n_sel.tolist() == [K]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("N,K", [(40, 9), (700, 60), (3001, 130)])
 @pytest.mark.parametrize("power", [-72, -66, -60])
 def test_selection_where_products_underflow(dtype, N, K, power):
