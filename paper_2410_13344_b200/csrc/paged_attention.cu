@@ -10,8 +10,8 @@
 //   - a warp per unit, many short sequences: nobody;
 //   - a cluster per unit: the warps of a CTA in shared memory, its CTAs in each other's;
 //   - shares, long caches: all units' pages one after another in equal parts, one per CTA of a single wave; units that were cut are joined by a second kernel.
-// 64 sequences of up to 8192 tokens (64 heads on 8, heads of 128, 1257 MB) 190 us and 4 for the join: 6.6 TB/s in the main kernel, the measured copy rate; CTAs of equal shares
-// end between 172 and 190.  One sequence of 1000 tokens (32 heads on 8) 5.0 us: 2.0 to the first keys' arrival, 0.4 for their products, 1.8 for the meeting.
+// 64 sequences of up to 8192 tokens (64 heads on 8, heads of 128, 1257 MB) 187 us and 4 for the join: 6.7 TB/s in the main kernel, the rate of a copy; CTAs of equal shares
+// end between 172 and 187.  One sequence of 1000 tokens (32 heads on 8) 5.0 us: 2.0 to the first keys' arrival, 0.4 for their products, 1.8 for the meeting.
 #include <math.h>
 #include <string.h>
 
@@ -338,7 +338,7 @@ __device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c
     }
 }
 
-// fp32, one or two heads to a unit, or four of 128: plain FMA.  (One head to a KV head: 123 MB in 20 us, 6.1 TB/s; 16 sequences of 8192 tokens, 4 heads on each of 8, 1074 MB: 164 us, 6.5 TB/s.)
+// fp32, one or two heads to a unit, or four of 128: plain FMA.  (One head to a KV head: 117 MB in 21 us, 5.6 TB/s; 16 sequences of 8192 tokens, 4 heads on each of 8, 1074 MB: 164 us, 6.5 TB/s.)
 // A lane owns DH / 32 elements of every key and value, a warp takes KEYS keys at a time for up to GH heads and has the next ones on their way.
 // The lanes' KEYS x GH partial sums meet by halving, after which each lane has the scores of few keys to take the exponential of; the weights come back by
 // shuffles.

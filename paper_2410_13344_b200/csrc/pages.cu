@@ -15,7 +15,7 @@ namespace {
 constexpr int PLAN_THREADS = 1024, PLAN_FEW = 256;
 constexpr int TRIM_CLUSTER = 8, TRIM_WIDE = 16;      // CTAs of a trim's cluster, of more requests than a CTA has threads
 // Up to this many rows one CTA fills them; more are spread over the SMs, and a second launch changes the state.
-// (64 requests of a token each: plan and trim 6.0 us; 300 requests, 11000 rows: 9.3; 2000 requests, a million rows, 45000 pages back: 19.)
+// (64 requests of a token each: plan and trim 5.2 us; 300 requests, 11000 rows: 9; 2000 requests, a million rows, 45000 pages back: 19.)
 constexpr int kPlanRowsAlone = 2048;
 constexpr int kMaxRequests = 8192;      // four words each of a CTA's shared memory
 
