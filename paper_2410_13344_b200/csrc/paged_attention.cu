@@ -889,6 +889,10 @@ constexpr int kFewPages = 4096;
 // Shares of fewer items cost more in joins than they save.  (1 unit of 64 pages, 4 / 8 / 16 items: 7.6 / 7.8 / 9.2 us; 64 of 24: 10.9 / 10.2 / 11.6.)
 // Of units that have fewer in the mean, a share takes one: else up to eight stand one behind another.  (512 units of a page, at most 512 by the caller's word, 20.9 -> 7.5 us.)
 constexpr int kMinShare = 8;
+// Clusters of so many CTAs that run at once, with this many CTAs to an SM: those of a cluster lie in one of the GPU's eight parts, whose SMs are no multiple of them.  One more, and the last run when
+// the first have ended.  (us, units of 60 pages: 32 / 34 in clusters of 8, two to an SM, 6.7 / 10.3; 46 / 50, three to an SM, 7.6 / 11.0; 14 / 16 in clusters of 16, two to an SM, 8.7 / 15.6;
+// 70 / 74 in clusters of 4, two to an SM, 8.7 / 13.6.)
+constexpr int clusters_at_once(int together, int per_sm) { return per_sm * (together == 16 ? 7 : together == 8 ? 16 : together == 4 ? 35 : 148 / together); }
 // max_items: pages that a sequence can have to be looked at (a window may begin and end inside one)
 int plan_paged(int dtype, int B, int H, int Hk, int head_dim, int max_len, int window, int max_sel, PagedPlan* g) {
   if (dtype != CERB_F32 && dtype != CERB_BF16) return CERB_E_ARG;
@@ -901,11 +905,15 @@ int plan_paged(int dtype, int B, int H, int Hk, int head_dim, int max_len, int w
   g->units_h = (G + g->heads_unit - 1) / g->heads_unit;
   g->units = (long long)B * Hk * g->units_h;
   if (g->units * std::max(g->heads_unit, PA_CLUSTER) > 0x7fffffffll) return CERB_E_SHAPE;
-  const int at_once = 148 * (bf ? (g->heads_unit == 8 ? ctas_per_sm<bf16, 64, 8>() : ctas_per_sm<bf16, 64, 16>())
-                                : g->heads_unit == 8 ? (head_dim == 64 ? ctas_per_sm<float, 64, 8>() : ctas_per_sm<float, 128, 8>())
-                                : g->heads_unit == 4 ? ctas_per_sm<float, 64, 4>() : ctas_per_sm<float, 64, 2>());
+  const int per_sm = bf ? (g->heads_unit == 8 ? ctas_per_sm<bf16, 64, 8>() : ctas_per_sm<bf16, 64, 16>())
+                        : g->heads_unit == 8 ? (head_dim == 64 ? ctas_per_sm<float, 64, 8>() : ctas_per_sm<float, 128, 8>())
+                        : g->heads_unit == 4 ? ctas_per_sm<float, 64, 4>() : ctas_per_sm<float, 64, 2>();
+  const int at_once = 148 * per_sm;
+  // (bf16, more units than seven: sixteen CTAs only where eight leave a warp many pages, us with 8 / 16: 8 units of 60 pages 5.2 / 5.6, of 200 7.9 / 8.1, of 400 11.9 / 10.7, of a list of 256 10.3 / 9.2; heads of 64, of 60
+  // 4.3 / 4.6, of 120 5.6 / 5.1)
+  const int widest = bf && g->units > 7 && items <= (head_dim == 64 ? 64 : 192) ? 8 : PA_CLUSTER;
   g->together = 1;
-  while (g->together < PA_CLUSTER && g->units * g->together * 2 <= at_once && g->together * 2 * PA_WARPS <= items + PA_WARPS) g->together *= 2;
+  while (g->together < widest && g->units <= clusters_at_once(2 * g->together, per_sm) && g->together * 2 * PA_WARPS <= items + PA_WARPS) g->together *= 2;
   if (g->units > at_once || items > (long long)g->together * PA_WARPS * (bf || g->heads_unit <= 2 || g->heads_unit * head_dim == 256 ? kClusterPages : kClusterPages / 2)) g->together = 0;
   g->min_share = kMinShare;
   if (g->units > at_once ? items <= 4 * kWarpPages : g->units * 2 > at_once && items <= kWarpPages) g->together = -1;
@@ -919,7 +927,7 @@ int plan_paged(int dtype, int B, int H, int Hk, int head_dim, int max_len, int w
     g->joins = 0;
     // while two CTAs to an SM are enough, and a warp has more than one page, the warps have the registers for two pages ahead (64 units of 32 / 64 pages 8.0 / 10.3 -> 6.6 / 8.4 us,
     // 128 of 32 / 64 10.5 / 16.7 -> 9.0 / 14.5; in shares, and with fewer CTAs to have it so: no gain)
-    g->deep = bf && g->ctas <= 2 * 148 && items > g->together * PA_WARPS * (128 / head_dim);
+    g->deep = bf && g->units <= clusters_at_once(g->together, 2) && items > g->together * PA_WARPS * (128 / head_dim);
     return CERB_OK;
   }
   const long long most = std::max(1ll, (g->units * items + g->min_share - 1) / g->min_share);
