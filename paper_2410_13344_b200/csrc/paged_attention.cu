@@ -11,7 +11,7 @@
 //   - a cluster per unit: the warps of a CTA in shared memory, its CTAs in each other's;
 //   - shares, long caches: all units' pages one after another in equal parts, one per CTA of a single wave; units that were cut are joined by a second kernel.
 // 64 sequences of up to 8192 tokens (64 heads on 8, heads of 128, 1257 MB) 187 us and 4 for the join: 6.7 TB/s in the main kernel, the rate of a copy; CTAs of equal shares
-// end between 172 and 187.  One sequence of 1000 tokens (32 heads on 8) 5.0 us: 2.0 to the first keys' arrival, 0.4 for their products, 1.8 for the meeting.
+// end between 172 and 187.  One sequence of 1000 tokens (32 heads on 8) 5.0 us a pass: 2.0 to the first keys' arrival, 0.4 for their products, the rest the meeting and the launch.
 #include <math.h>
 #include <string.h>
 
@@ -872,7 +872,7 @@ struct PagedPlan {
   bool deep;                                                             // two pages of a warp ahead, in a cluster
   long long units;
 };
-// A cluster per unit, as many CTAs as make the grid one wave and find a page for each of their warps, while the longest sequence leaves a warp no more than 12 pages;
+// A cluster per unit, as many CTAs as let all run at once and find a page for each of their warps, while the longest sequence leaves a warp no more than 12 pages;
 // shares and a join beyond that.  (bf16, 4 x 8 heads of 128, all sequences alike / between half as long and as long, every fourth idle; us with
 // clusters, with shares: 64 units of 8 pages 5.8 / 5.8, 7.0 / 13.0; 8 of 400 11.4 / 9.6, 13.4 / 15.2; 192 of 64 19.7 / 17.9, 23.3 / 19.5; 1 of 400 8.4, 9.8.  More than
 // that to a warp, the longest decide: 256 units of 64 29.6 / 27.9, 28.2 / 21.8; 128 of 160 35.8 / 32.2, 36.4 / 24.3; 1 of 1000 14.1, 10.6.  And of more than one wave: 512 units
