@@ -473,6 +473,18 @@ def test_selection_with_an_infinity_or_nan_on_the_side_that_does_not_count(dtype
     check_lists(sel, n_sel, want, K)
 
 
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("N", [60, 700])
+def test_fp32_selection_with_queries_that_are_not_finite(bad, N):
+    lo, hi = score_cache("plain", "fp32", N)
+    lo[5, :, 5] = hi[5, :, 5] = 0.0
+    table, lens = torch.arange(N, dtype=torch.int32)[None].repeat(2, 1), [N * PAGE, N * PAGE - 3]
+    q = torch.randn(2, 12, 64, generator=torch.Generator().manual_seed(1))
+    q[1, 7, 5] = bad
+    sel, n_sel = binding.page_select(q.cuda(), lo.cuda(), hi.cuda(), table.cuda(), i32(lens), 50, N * PAGE)
+    check_lists(sel, n_sel, ref.select(q, lo, hi, table, lens, 50), 50)
+
+
 def test_selection_with_queries_that_are_not_finite_and_pages_outside_the_pool():
     lo, hi = score_cache("plain", "bf16", 500)
     table = torch.arange(500, dtype=torch.int32)[None].repeat(2, 1)
