@@ -547,8 +547,8 @@ __global__ void __launch_bounds__(SEL_THREADS, 1024 / SEL_THREADS) page_select_k
   } else if (!all_again && want > 0) {
 #pragma unroll 1
     for (int level = 0; level < 8; ++level) {
-      const float inv = (float)SEL_BINS / (hi - lo);
-      if (!(hi > lo) || !(inv < INFINITY)) break;
+      const float range = hi - lo, inv = (float)SEL_BINS / range;
+      if (!(hi > lo) || !(range < INFINITY) || !(inv < INFINITY)) break;    // (finite scores further apart than fp32 reaches: all of them are near)
       auto bin_of = [&](float s) { return min(SEL_BINS - 1, max(0, (int)((s - lo) * inv))); };
       if (level) {
         __syncthreads();

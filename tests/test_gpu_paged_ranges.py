@@ -1,0 +1,53 @@
+"""Paged-cache operators at the ends of their ranges, against the plain implementations in 64 bits (paged_reference.py)."""
+import random
+
+import pytest
+import torch
+
+import paged_reference as ref
+from paper_2410_13344_b200 import binding
+
+pytestmark = pytest.mark.gpu
+PAGE = 16
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def check_lists(sel, n_sel, want, K):
+    for b, rows in enumerate(want):
+        assert int(n_sel[b]) == len(rows[0])
+        for h, row in enumerate(rows):
+            assert sel[b, h].tolist() == row + [-1] * (K - len(row)), (b, h)
+
+
+# ---------------------------------------------------------------------------------------------- selection
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("N,G,K", [(20, 8, 4), (34, 4, 20), (34, 4, 9), (40, 4, 9), (300, 2, 60), (3001, 3, 130)])
+@pytest.mark.parametrize("kind", ["one each", "both ways", "one side"])
+def test_selection_where_finite_scores_span_more_than_fp32_holds(dtype, N, G, K, kind):
+    g = torch.Generator().manual_seed(N)
+    mid, spread = torch.randn(N, 1, 64, generator=g), torch.rand(N, 1, 64, generator=g)
+    lo, hi = mid - spread, mid + spread
+    # one channel, in which every query is 1: scores stay finite
+    if kind == "one each":
+        lo[N // 3, 0, 9] = hi[N // 3, 0, 9] = 3e38
+        lo[N // 2, 0, 9] = hi[N // 2, 0, 9] = -3e38
+    else:
+        size = 2e38 + 1.2e38 * torch.rand(N, generator=g)
+        sign = torch.where(torch.rand(N, generator=g) < 0.5, -1.0, 1.0) if kind == "both ways" else 1.0
+        lo[:, 0, 9] = hi[:, 0, 9] = size * sign
+    lo, hi = lo.to(DT[dtype]), hi.to(DT[dtype])
+    q = torch.randn(1, G, 64, generator=torch.Generator().manual_seed(1)).to(DT[dtype])
+    q[:, :, 9] = 1.0
+    table = torch.tensor([random.Random(N).sample(range(N), N)], dtype=torch.int32)
+    x, at = q[0].double(), table[0].long()
+    scores = (x.clamp(min=0) @ hi[at, 0].double().T + x.clamp(max=0) @ lo[at, 0].double().T).float()
+    assert bool(torch.isfinite(scores).all())
+    assert kind == "one side" or bool(torch.isinf(scores.amax() - scores.amin()))
+    sel, n_sel = binding.page_select(q.cuda(), lo.cuda(), hi.cuda(), table.cuda(), i32([N * PAGE]), K, N * PAGE)
+    check_lists(sel, n_sel, ref.select(q, lo, hi, table, [N * PAGE], K), K)
