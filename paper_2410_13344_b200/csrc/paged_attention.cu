@@ -164,8 +164,9 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
 // out^T = V^T P^T.  The order of the k positions of a product is free as long as both operands have the same, so a lane's 16
 // bytes of a key row (8 consecutive elements) are what it needs of two MMAs, and what it loads of the values, 8 elements of each of four keys, is
 // interleaved into fragments by byte permutes.  S^T's sums become P^T's fragments by 8 x 8 transpositions of 16-bit elements.
-// P is rounded to bf16 for the second product (each weight off by at most 2^-8 of itself, up or down; the sum l is that of the unrounded
-// ones); scores, maxima, sums and outputs are fp32.
+// P enters the second product as two bf16 terms, itself rounded and what that leaves, as in tree attention: a weight is off by at most 2^-16 of itself, and the sum l is that of the unrounded
+// ones; scores, maxima, sums and outputs are fp32.  (With one term a weight is off by up to 2^-8.  The second costs, us with one / two: 64 sequences of up to 8192 tokens 193.8 / 194.1, one of 1000
+// 5.6 / 5.7, 128 of 2000 with heads of 64 55.4 / 56.4, 16 of 4096 with 16 heads to a unit 26.9 / 27.4, 24 selections of 128 pages 65.6 / 65.9 with the selection.)
 // A warp takes KP pages at a time, 8 KB of keys and values, and has the next AHEAD times as many on their way.
 template <int DH, int NT, int AHEAD>
 __device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c, Sums<DH, 8 * NT>& sums) {
@@ -265,7 +266,7 @@ __device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c
           }
         }
       }
-      uint32_t pb[KP][NT][2];
+      uint32_t pb[KP][NT][2], pl[KP][NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         float mx[2] = {fmaxf(s[0][n][0], s[0][n][2]), fmaxf(s[0][n][1], s[0][n][3])};
@@ -300,8 +301,12 @@ __device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c
         }
 #pragma unroll
         for (int a = 0; a < KP; ++a) {
-          pb[a][n][0] = transpose8x8(pack_bf16(s[a][n][0], s[a][n][1]));
-          pb[a][n][1] = transpose8x8(pack_bf16(s[a][n][2], s[a][n][3]));
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t hi = pack_bf16(s[a][n][2 * e], s[a][n][2 * e + 1]);
+            pb[a][n][e] = transpose8x8(hi);
+            pl[a][n][e] = transpose8x8(pack_bf16(s[a][n][2 * e] - __uint_as_float(hi << 16), s[a][n][2 * e + 1] - __uint_as_float(hi & 0xffff0000u)));
+          }
         }
       }
 #pragma unroll
@@ -315,7 +320,10 @@ __device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c
             const uint32_t a0 = __byte_perm(x[0][d], x[1][d], 0x5410), a1 = __byte_perm(x[0][d], x[1][d], 0x7632);
             const uint32_t a2 = __byte_perm(x[2][d], x[3][d], 0x5410), a3 = __byte_perm(x[2][d], x[3][d], 0x7632);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) mma_16816(o[n][4 * j + d], a0, a1, a2, a3, pb[a][n][0], pb[a][n][1]);
+            for (int n = 0; n < NT; ++n) {
+              mma_16816(o[n][4 * j + d], a0, a1, a2, a3, pb[a][n][0], pb[a][n][1]);
+              mma_16816(o[n][4 * j + d], a0, a1, a2, a3, pl[a][n][0], pl[a][n][1]);
+            }
           }
         }
       if (then[0].at >= 0) load_v(v, then);
