@@ -86,7 +86,7 @@ __device__ __forceinline__ Share share_of(int B, F items, int index, int shares,
   }
   const long long total = __shfl_sync(0xffffffffu, sum, 31);
   Share s;
-  const long long even = total >> 32 ? (total + shares - 1) / shares : ((unsigned)total + (unsigned)(shares - 1)) / (unsigned)shares;
+  const long long even = total >> 32 ? (total + shares - 1) / shares : (unsigned)total / (unsigned)shares + ((unsigned)total % (unsigned)shares != 0);
   s.size = max(even, total >= min_share * units ? (long long)min_share : (long long)max(1u, (unsigned)total / (unsigned)units));
   s.begin = min(total, s.size * index);
   s.end = min(total, s.begin + s.size);

@@ -51,3 +51,22 @@ def test_selection_where_finite_scores_span_more_than_fp32_holds(dtype, N, G, K,
     assert kind == "one side" or bool(torch.isinf(scores.amax() - scores.amin()))
     sel, n_sel = binding.page_select(q.cuda(), lo.cuda(), hi.cuda(), table.cuda(), i32([N * PAGE]), K, N * PAGE)
     check_lists(sel, n_sel, ref.select(q, lo, hi, table, [N * PAGE], K), K)
+
+
+# ---------------------------------------------------------------------------------------------- attention
+
+
+def test_attention_over_lists_of_nearly_2_to_the_32_entries():
+    """Four thousand heads share a list of 2^24 - 1 entries, of which twenty are pages: 256 units, 2^32 - 256 items in all."""
+    H, D, K, length = 4096, 64, (1 << 24) - 1, 16 * 20 - 3
+    g = torch.Generator().manual_seed(1)
+    k_pool, v_pool = (torch.randn(20, 1, PAGE, D, generator=g).bfloat16() for _ in range(2))
+    q = torch.randn(1, H, D, generator=g).bfloat16()
+    table = torch.randperm(20, generator=g).to(torch.int32)[None]
+    sel = torch.full((1, 1, K), -1, dtype=torch.int32)
+    at = random.Random(1).sample(range(K), 16) + [0, K - 1, K // 2, 14510163]
+    assert len(set(at)) == 20
+    sel[0, 0, at] = torch.arange(20, dtype=torch.int32)
+    out, lse = binding.paged_attention(q.cuda(), k_pool.cuda(), v_pool.cuda(), table.cuda(), i32([length]), 0.125, 1 << 28, sel=sel.cuda(), n_sel=i32([K]))
+    o, l, (to, tl) = ref.attention(q, k_pool, v_pool, table, [length], 0.125)
+    assert bool(((out.double().cpu() - o).abs() <= to).all()) and bool(((lse.double().cpu() - l).abs() <= tl).all())
