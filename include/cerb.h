@@ -363,7 +363,7 @@ int cerb_kv_append(const cerb_kv_append_args* args, void* stream);
  * out[b][h] = softmax over s of scale * q[b][h] . k[s], times v[s], with the KV head h / (n_heads / n_kv_heads); s are the
  * slots max(0, len[b] - window) .. len[b] - 1 (window 0: all), with a list those of them in the pages that it names: sel[b][kv head][i], i < n_sel[b],
  * logical pages in any order, entries outside the sequence count nothing, a page that comes twice counts twice.  No slots: out 0, lse -infinity.
- * lse = natural log of the softmax denominator.  Any n_heads divisible by n_kv_heads. */
+ * lse = natural log of the softmax denominator.  Any n_heads divisible by n_kv_heads.  CERB_E_SHAPE: max_sel above 2^30. */
 typedef struct cerb_paged_attn_args {
   int32_t dtype;                /* CERB_BF16 | CERB_F32 */
   int32_t B, n_heads, n_kv_heads, head_dim;     /* head_dim 64 or 128 */
@@ -393,7 +393,8 @@ int cerb_paged_attention(const cerb_paged_attn_args* args, void* stream);
  * n_last <= max_sel), then the best scores, until max_sel are; all of a sequence of max_sel pages or fewer.  Decisions are made in
  * exact arithmetic, up to the rounding of sums of fp64; equal scores: the lower page; a score that is not a number counts as infinity.
  * sel: logical pages in ascending order, -1 behind the last one; n_sel[b] = min(pages of b, max_sel).
- * CERB_E_SHAPE: max_pages above 131072 (2 097 152 tokens), more than 64 query heads to a KV head, 2^16 KV heads or more, B * n_kv_heads of 2^23 or more. */
+ * CERB_E_SHAPE: max_pages above 131072 (2 097 152 tokens), more than 64 query heads to a KV head, 2^16 KV heads or more, B * n_kv_heads of 2^23 or more,
+ * max_sel above 2^30. */
 typedef struct cerb_page_select_args {
   int32_t dtype;                /* CERB_BF16 | CERB_F32 */
   int32_t B, n_heads, n_kv_heads, head_dim;     /* head_dim 64 or 128 */

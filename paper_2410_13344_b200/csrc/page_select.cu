@@ -723,7 +723,7 @@ int cerb_page_select_scratch_bytes(int32_t dtype, int32_t B, int32_t n_heads, in
 int cerb_page_select(const cerb_page_select_args* a, void* stream) {
   if (!a || (a->B > 0 && (!a->q || !a->k_min || !a->k_max || !a->page_table || !a->len || !a->sel || !a->n_sel))) return CERB_E_ARG;
   if (a->n_pool_pages < 1 || a->max_len < 1 || a->n_first < 0 || a->n_last < 0 || a->max_sel < 1) return CERB_E_ARG;
-  if ((long long)a->n_first + a->n_last > a->max_sel) return CERB_E_SHAPE;
+  if ((long long)a->n_first + a->n_last > a->max_sel || a->max_sel > kMaxList) return CERB_E_SHAPE;
   SelectPlan g;
   CERB_TRY(plan_select(a->dtype, a->B, a->n_heads, a->n_kv_heads, a->head_dim, a->max_pages, a->max_len, &g));
   const int es = a->dtype == CERB_BF16 ? 2 : 4;

@@ -904,7 +904,7 @@ constexpr int clusters_at_once(int together, int per_sm) { return per_sm * (toge
 // max_items: pages that a sequence can have to be looked at (a window may begin and end inside one)
 int plan_paged(int dtype, int B, int H, int Hk, int head_dim, int max_len, int window, int max_sel, PagedPlan* g) {
   if (dtype != CERB_F32 && dtype != CERB_BF16) return CERB_E_ARG;
-  if (B < 0 || H < 1 || Hk < 1 || H % Hk || (head_dim != 64 && head_dim != 128)) return CERB_E_SHAPE;
+  if (B < 0 || H < 1 || Hk < 1 || H % Hk || (head_dim != 64 && head_dim != 128) || max_sel > kMaxList) return CERB_E_SHAPE;
   const long long whole = ((long long)max_len + CERB_PAGE - 1) / CERB_PAGE, in_window = ((long long)window + 2 * CERB_PAGE - 2) / CERB_PAGE;
   const long long items = max_sel > 0 ? std::min((long long)max_sel, whole) : window > 0 && in_window < whole ? in_window : whole;
   const int G = H / Hk;

@@ -1,9 +1,11 @@
-// Shared by the kernels that read a paged cache for one new token.  Device code only.
+// Shared by the kernels that read a paged cache for one new token.
 #pragma once
 
 #include "cerb_internal.cuh"
 
 namespace cerb {
+
+constexpr int kMaxList = 1 << 30;       // entries of a list of pages: its indices are ints that step past its end
 
 // 16 bytes that are read once.  (Not through the read-only path: kernels in front may have written them.)
 __device__ __forceinline__ uint4 ld16(const void* src) {
