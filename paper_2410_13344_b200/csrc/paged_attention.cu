@@ -657,7 +657,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32, ctas_per_sm<T, DH, HEADS>()) pa
   // sequences without anything to look at
   for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
     if (span_of(p, b).items) continue;
-    for (int i = threadIdx.x; i < p.H * DH; i += PA_WARPS * 32) store_out<T>(p, (size_t)b * p.H + i / DH, i % DH, DH, 0.f);
+    for (size_t i = threadIdx.x; i < (size_t)p.H * DH; i += PA_WARPS * 32) store_out<T>(p, (size_t)b * p.H + i / DH, (int)(i % DH), DH, 0.f);
     for (int i = threadIdx.x; i < p.H; i += PA_WARPS * 32) store_lse(p, (size_t)b * p.H + i, -INFINITY, 0.f);
     if (p.by_unit)
       for (int i = threadIdx.x; i < uh; i += PA_WARPS * 32) p.meta[b * uh + i] = make_int4(0, 0, 0, 0);

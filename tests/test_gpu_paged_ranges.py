@@ -70,3 +70,15 @@ def test_attention_over_lists_of_nearly_2_to_the_32_entries():
     out, lse = binding.paged_attention(q.cuda(), k_pool.cuda(), v_pool.cuda(), table.cuda(), i32([length]), 0.125, 1 << 28, sel=sel.cuda(), n_sel=i32([K]))
     o, l, (to, tl) = ref.attention(q, k_pool, v_pool, table, [length], 0.125)
     assert bool(((out.double().cpu() - o).abs() <= to).all()) and bool(((lse.double().cpu() - l).abs() <= tl).all())
+
+
+def test_an_idle_sequence_of_2_to_the_31_outputs():
+    H, D = 1 << 24, 128
+    q = torch.ones(1, 1, D, dtype=torch.bfloat16, device="cuda").expand(1, H, D)
+    pool = torch.ones(1, 1, PAGE, D, dtype=torch.bfloat16, device="cuda")
+    before = torch.full((6 << 30,), 255, dtype=torch.uint8, device="cuda")                  # (what the results' memory may hold)
+    del before
+    out, lse = binding.paged_attention(q, pool, pool, i32([[0]]), i32([0]), 0.1, 60000)
+    assert not bool(out.view(torch.int16).any()) and bool(torch.isneginf(lse).all())
+    del out, lse
+    torch.cuda.empty_cache()
