@@ -252,17 +252,17 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) pages_trim_kernel(const Pages
   }
   cluster_arrive();
   __syncthreads();
-  // two pages to a lane
-  for (int w0 = 2 * (int)(cta * PLAN_THREADS + (tid & ~31)); w0 < total; w0 += 2 * (int)(ctas * PLAN_THREADS)) {
-    int b = find_request(ends, p.B, w0), page[2];
+  // two pages to a lane  (counted in 32 bits without a sign: up to 2^31 of them, and a step past the last)
+  for (unsigned w0 = 2 * (cta * PLAN_THREADS + (tid & ~31)); w0 < (unsigned)total; w0 += 2 * ctas * PLAN_THREADS) {
+    int b = find_request(ends, p.B, (int)w0), page[2];
     int32_t* entry[2] = {nullptr, nullptr};
-    const bool one = ends[b] > w0 + 63;
+    const bool one = (unsigned)ends[b] > w0 + 63;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int at = w0 + 32 * i + (tid & 31);
-      if (at >= total) continue;
-      const int c = one ? b : find_near(ends, p.B, b, at);
-      entry[i] = p.page_table + (size_t)c * p.max_pages + pages_of(news[c]) + at - (c ? ends[c - 1] : 0);
+      const unsigned at = w0 + 32 * i + (tid & 31);
+      if (at >= (unsigned)total) continue;
+      const int c = one ? b : find_near(ends, p.B, b, (int)at);
+      entry[i] = p.page_table + (size_t)c * p.max_pages + pages_of(news[c]) + ((int)at - (c ? ends[c - 1] : 0));
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) pages_trim_kernel(const Pages
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       if (entry[i]) {
-        const unsigned to = (unsigned)n_free + (unsigned)total - 1 - (unsigned)(w0 + 32 * i + (tid & 31));       // (less than 2^32)
+        const unsigned to = (unsigned)n_free + (unsigned)total - 1 - (w0 + 32 * i + (tid & 31));       // (less than 2^32)
         if (to < (unsigned)p.free_cap) p.free_pages[to] = page[i];
         *entry[i] = -1;
       }

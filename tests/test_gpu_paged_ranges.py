@@ -82,3 +82,24 @@ def test_an_idle_sequence_of_2_to_the_31_outputs():
     assert not bool(out.view(torch.int16).any()) and bool(torch.isneginf(lse).all())
     del out, lse
     torch.cuda.empty_cache()
+
+
+# ---------------------------------------------------------------------------------------------- pages
+
+
+def test_trim_of_nearly_2_to_the_31_pages():
+    B, each = 33, 65075262
+    total = B * each                                        # 2^31 - 2
+    table = torch.arange(total, dtype=torch.int32, device="cuda").remainder_(1 << 27).view(B, each)
+    free = torch.full((total + 1,), -5, dtype=torch.int32, device="cuda")
+    lens, n_free = i32([each * PAGE] * B), i32([1])
+    binding.pages_trim(i32([0] * B), lens, table, free, n_free)
+    assert n_free.tolist() == [total + 1] and not bool(lens.any()) and int(free[0]) == -5
+    assert bool((table == -1).all())
+    del table
+    for lo in range(0, total, 1 << 28):                     # page i of the table lies total - i above the bottom
+        hi = min(total, lo + (1 << 28))
+        want = torch.arange(lo, hi, dtype=torch.int32, device="cuda").remainder_(1 << 27)
+        assert torch.equal(free[total - hi + 1:total - lo + 1].flip(0), want)
+    del free
+    torch.cuda.empty_cache()
