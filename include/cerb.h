@@ -334,13 +334,15 @@ typedef struct cerb_pages {
  * including it (by requests that fit) are there; a request that needs no new page needs no page to be there.  Otherwise it gets none.
  * granted dev [B]: n_new or 0.  len and n_free change accordingly.  slot, pos, seq dev [rows]: of row r of a granted request its physical slot
  * (page * 16 + row of the page), its position (len + r - row_off[b]) and the request; -1 for other rows and behind the last one.
+ * The first n_free entries of free_pages must be pages: whatever stands there is handed out (and a slot of what can be no page is negative).
  * CERB_E_SHAPE: more than 8192 requests, B * max_pages of 2^31 or more, more than 2^30 rows. */
 int cerb_pages_plan(const cerb_pages* state, const int32_t* n_new, int32_t rows, int32_t* slot, int32_t* pos, int32_t* seq,
                     int32_t* row_off, int32_t* granted, void* stream);
 
 /* Cuts every request down to keep[b] tokens (dev [B]; more than it has = it stays as it is; 0 = it is done) and gives back the pages that
  * it then does not need; their table entries become -1.  The last page of the last request is given back first, so that a trim to
- * the lengths before a plan restores the stack.  Pages that the stack has no room for are dropped. */
+ * the lengths before a plan restores the stack.  Table entries that can be no page (negative, or 2^27 and above: of pages behind a window, say, that were given back by hand) are
+ * passed over.  Pages that the stack has no room for are dropped; what stands above its top is undefined. */
 int cerb_pages_trim(const cerb_pages* state, const int32_t* keep, void* stream);
 
 /* Writes a step's keys and values into their slots.  With k_min and k_max (both or neither), element-wise minimum and maximum of the keys of a

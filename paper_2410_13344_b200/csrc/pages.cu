@@ -15,7 +15,7 @@ namespace {
 constexpr int PLAN_THREADS = 1024, PLAN_FEW = 256;
 constexpr int TRIM_CLUSTER = 8, TRIM_WIDE = 16;      // CTAs of a trim's cluster, of more requests than a CTA has threads
 // Up to this many rows one CTA fills them; more are spread over the SMs, and a second launch changes the state.
-// (64 requests of a token each: plan and trim 5.2 us; 300 requests, 11000 rows: 9; 2000 requests, a million rows, 45000 pages back: 19.)
+// (64 requests of a token each: plan and trim 6.0 us; 300 requests, 11000 rows: 9.3; 2000 requests, a million rows, 45000 pages back: 20.5.)
 constexpr int kPlanRowsAlone = 2048;
 constexpr int kMaxRequests = 8192;      // four words each of a CTA's shared memory
 
@@ -30,6 +30,9 @@ __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 __device__ __forceinline__ int pages_of(int tokens) { return (int)(((unsigned)tokens + CERB_PAGE - 1) / CERB_PAGE); }
+
+// What a table or the stack may name as a page: those of a pool of less than 2^27 of them.
+__device__ __forceinline__ bool can_be_page(int page) { return (unsigned)page < 1u << 27; }
 
 // A slot of what a table or the stack names as a page.  (What can be no page, of a pool of less than 2^27 of them, gives a slot that nothing is written to.)
 __device__ __forceinline__ int slot_of(int page, int row) { return page >= 1 << 27 ? -1 : max(page, -(1 << 27)) * CERB_PAGE + row; }
@@ -233,12 +236,16 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) pages_grant_kernel(const Page
 
 // Pages behind the lengths to keep go back to the list, the last one of the last request first: a trim to the lengths before a
 // plan leaves the list as it was.  One cluster: lengths and free count change behind its barrier.
+// Table entries that can be no page (of a window's old pages, say, which were given back by hand) are passed over.  They are found as the pages are written, and then the first CTA closes the gaps that
+// they have left; where the stack may not have room for all, it goes through the entries by itself.  (Trim and plan of 64 requests 5.9 us without looking for them, 6.0 with; of 2000, 45000 entries,
+// 19.7 and 20.5, another barrier of the cluster; counting them before anything is written 6.7 and 21.2.  With gaps: 4000 entries 6.7 us instead of 3.9, 44000 36 instead of 8, and 74 without room.)
 __global__ void __launch_bounds__(PLAN_THREADS, 1) pages_trim_kernel(const PagesParams p) {
   extern __shared__ __align__(16) int sm[];
   int *ends = sm, *news = ends + p.B;                          // pages given back before and of b; the length kept
-  __shared__ int red_pages[32];
+  __shared__ int red_pages[32], s_some;
   const int tid = threadIdx.x;
   const unsigned cta = blockIdx.x, ctas = gridDim.x;                 // (one cluster)
+  if (tid == 0) s_some = 0;
   griddep_wait();
   const int n_free = min(max(*p.n_free, 0), p.free_cap);
   int total = 0;
@@ -252,8 +259,10 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) pages_trim_kernel(const Pages
   }
   cluster_arrive();
   __syncthreads();
+  const bool room = (unsigned)n_free + (unsigned)total <= (unsigned)p.free_cap;
+  bool some = !room;                                                     // (which of them fit, if any are no page, is seen one after another)
   // two pages to a lane  (counted in 32 bits without a sign: up to 2^31 of them, and a step past the last)
-  for (unsigned w0 = 2 * (cta * PLAN_THREADS + (tid & ~31)); w0 < (unsigned)total; w0 += 2 * ctas * PLAN_THREADS) {
+  for (unsigned w0 = 2 * (cta * PLAN_THREADS + (tid & ~31)); room && w0 < (unsigned)total; w0 += 2 * ctas * PLAN_THREADS) {
     int b = find_request(ends, p.B, (int)w0), page[2];
     int32_t* entry[2] = {nullptr, nullptr};
     const bool one = (unsigned)ends[b] > w0 + 63;
@@ -270,15 +279,50 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) pages_trim_kernel(const Pages
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       if (entry[i]) {
-        const unsigned to = (unsigned)n_free + (unsigned)total - 1 - (w0 + 32 * i + (tid & 31));       // (less than 2^32)
-        if (to < (unsigned)p.free_cap) p.free_pages[to] = page[i];
+        some |= !can_be_page(page[i]);
+        p.free_pages[(unsigned)n_free + (unsigned)total - 1 - (w0 + 32 * i + (tid & 31))] = page[i];
         *entry[i] = -1;
       }
   }
+  some = __syncthreads_or(some);
   cluster_wait();
+  for (int b = tid; cta == 0 && b < p.B; b += PLAN_THREADS) p.len[b] = news[b];
+  if ((unsigned)total > 2 * PLAN_THREADS) {                              // (fewer are the first CTA's)
+    if (some && tid == 0) {
+      uint32_t at;
+      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(&s_some)), "r"(0));
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(1) : "memory");
+    }
+    cluster_arrive();
+    cluster_wait();
+    some = s_some;
+  }
   if (cta != 0) return;
-  for (int b = tid; b < p.B; b += PLAN_THREADS) p.len[b] = news[b];
-  if (tid == 0) *p.n_free = (int)min((unsigned)n_free + (unsigned)total, (unsigned)p.free_cap);
+  unsigned top = (unsigned)n_free + (unsigned)total;
+  if (some) {
+    // from the bottom of what is given back upwards: the entries themselves, or what has been written of them
+    top = n_free;
+    for (unsigned i0 = 0; i0 < (unsigned)total; i0 += PLAN_THREADS) {
+      const unsigned i = i0 + tid;
+      int page = -1;
+      if (i < (unsigned)total) {
+        if (room) {
+          page = p.free_pages[(unsigned)n_free + i];
+        } else {
+          const int at = (int)((unsigned)total - 1 - i), b = find_near(ends, p.B, 0, at);
+          int32_t* entry = p.page_table + (size_t)b * p.max_pages + pages_of(news[b]) + (at - (b ? ends[b - 1] : 0));
+          page = *entry;
+          *entry = -1;
+        }
+      }
+      const bool is = can_be_page(page);
+      int sum;
+      const unsigned to = top + block_scan<PLAN_THREADS>((int)is, red_pages, sum) - 1;
+      if (is && to < (unsigned)p.free_cap) p.free_pages[to] = page;
+      top += sum;
+    }
+  }
+  if (tid == 0) *p.n_free = (int)min(top, (unsigned)p.free_cap);
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -103,3 +103,45 @@ def test_trim_of_nearly_2_to_the_31_pages():
         assert torch.equal(free[total - hi + 1:total - lo + 1].flip(0), want)
     del free
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("B,max_pages,context,gone", [(1, 3, 40, 1.0), (3, 8, 120, 0.5), (40, 30, 450, 0.3), (300, 60, 900, 0.02), (2049, 40, 600, 0.5), (5, 9000, 140000, 0.4), (3, 9000, 140000, 0.0002),
+                                                      (1200, 50, 700, 0.0)])
+def test_trim_passes_over_entries_that_are_no_page(B, max_pages, context, gone):
+    """Requests whose old pages have been given back by hand, as behind a window: the stack has room for every page once, and gets every page once."""
+    rng = random.Random(B * 7 + max_pages)
+    lens = [rng.choice([0, context, rng.randint(0, context)]) for _ in range(B)]
+    lens[-1] = context
+    held = [ref.pages_of(n) for n in lens]
+    n_pages = sum(held) + 50
+    pool = rng.sample(range(n_pages), n_pages)
+    table = [[pool.pop() for _ in range(h)] + [-1] * (max_pages - h) for h in held]
+    free = pool
+    for b, h in enumerate(held):
+        for j in range(h - 1):
+            if rng.random() < gone:
+                free.append(table[b][j])
+                table[b][j] = rng.choice([-1, -1, -2 ** 31, 2 ** 27, 2 ** 31 - 1])
+    n_free = len(free)
+    free = free + [-3] * (n_pages - n_free)
+    state = [i32(lens), i32(table).view(B, max_pages), i32(free), i32([n_free])]
+    for keep in ([rng.choice([n, max(0, n - 3), rng.randint(0, n), n // 2]) for n in lens], [0] * B):
+        binding.pages_trim(i32(keep), *state)
+        back = []
+        for b, n in enumerate(keep):
+            n = min(n, lens[b])
+            for j in range(ref.pages_of(n), ref.pages_of(lens[b])):
+                if 0 <= table[b][j] < 2 ** 27:
+                    back.append(table[b][j])
+                table[b][j] = -1
+            lens[b] = n
+        free[n_free:n_free + len(back)] = back[::-1]
+        n_free += len(back)
+        assert state[0].tolist() == lens and state[1].tolist() == table and state[3].tolist() == [n_free]
+        assert state[2].tolist()[:n_free] == free[:n_free]
+        # what a plan then hands out are pages
+        new = [1] * B
+        plan = binding.pages_plan(i32(new), *[t.clone() for t in state], B)
+        whole = [b for b in range(B) if lens[b] % PAGE == 0 and int(plan.granted[b])] if B < 50 else []
+        assert all(int(plan.slot[b]) >= 0 for b in whole)
+    assert sorted(free) == list(range(n_pages))
