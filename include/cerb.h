@@ -332,7 +332,7 @@ typedef struct cerb_pages {
  * of the step's buffers (row_off dev [B+1]: the exclusive sums of n_new).  In the order of the requests: a request gets its tokens, and the
  * new pages they need from the top of the stack on, if they fit its table row and end within `rows` rows and the pages wanted up to and
  * including it (by requests that fit) are there; a request that needs no new page needs no page to be there.  Otherwise it gets none.
- * granted dev [B]: n_new or 0.  len and n_free change accordingly.  slot, pos, seq dev [rows]: of row r of a granted request its physical slot
+ * granted dev [B]: n_new or 0.  n_free and the lengths of requests that get tokens change accordingly.  slot, pos, seq dev [rows]: of row r of a granted request its physical slot
  * (page * 16 + row of the page), its position (len + r - row_off[b]) and the request; -1 for other rows and behind the last one.
  * The first n_free entries of free_pages must be pages: whatever stands there is handed out (and a slot of what can be no page is negative).
  * CERB_E_SHAPE: more than 8192 requests, B * max_pages of 2^31 or more, more than 2^30 rows. */

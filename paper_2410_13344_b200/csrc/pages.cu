@@ -215,8 +215,10 @@ __global__ void __launch_bounds__(THREADS, 1) pages_plan_kernel(const PagesParam
     }
   }
   if (!ALONE) return;
-  for (int b = tid; b < p.B; b += THREADS)
-    if (give[b]) p.len[b] = lens[b] + ends[b] - (b ? ends[b - 1] : 0);
+  for (int b = tid; b < p.B; b += THREADS) {
+    const int n = ends[b] - (b ? ends[b - 1] : 0);
+    if (give[b] && n) p.len[b] = lens[b] + n;
+  }
   if (tid == 0) *p.n_free = n_free - s_taken;
 }
 

@@ -145,3 +145,12 @@ def test_trim_passes_over_entries_that_are_no_page(B, max_pages, context, gone):
         whole = [b for b in range(B) if lens[b] % PAGE == 0 and int(plan.granted[b])] if B < 50 else []
         assert all(int(plan.slot[b]) >= 0 for b in whole)
     assert sorted(free) == list(range(n_pages))
+
+
+@pytest.mark.parametrize("rows", [4, 600, 5000])              # one CTA of few threads, one of many, many CTAs
+def test_a_plan_changes_the_lengths_of_those_that_get_tokens(rows):
+    lens, table = i32([-5, 1000, 20, 7, -5, 1000]), i32([[-1] * 3, [5, 6, 7], [8, 9, -1], [10, -1, -1], [-1] * 3, [11, 12, 13]])
+    free, n_free = i32([1, 2, 3]), i32([100])
+    plan = binding.pages_plan(i32([0, 0, 0, 1, 1, 1]), lens, table, free, n_free, rows)
+    assert plan.granted.tolist() == [0, 0, 0, 1, 1, 0] and plan.slot.tolist() == [10 * 16 + 7, 3 * 16, -1] + [-1] * (rows - 3)
+    assert lens.tolist() == [-5, 1000, 20, 8, 1, 1000] and n_free.tolist() == [2]
