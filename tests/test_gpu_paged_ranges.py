@@ -1,4 +1,5 @@
 """Paged-cache operators at the ends of their ranges, against the plain implementations in 64 bits (paged_reference.py)."""
+import math
 import random
 
 import pytest
@@ -6,6 +7,7 @@ import torch
 
 import paged_reference as ref
 from paper_2410_13344_b200 import binding
+from test_gpu_paged import score_cache
 
 pytestmark = pytest.mark.gpu
 PAGE = 16
@@ -51,6 +53,37 @@ def test_selection_where_finite_scores_span_more_than_fp32_holds(dtype, N, G, K,
     assert kind == "one side" or bool(torch.isinf(scores.amax() - scores.amin()))
     sel, n_sel = binding.page_select(q.cuda(), lo.cuda(), hi.cuda(), table.cuda(), i32([N * PAGE]), K, N * PAGE)
     check_lists(sel, n_sel, ref.select(q, lo, hi, table, [N * PAGE], K), K)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("kind", ["plain", "equal", "zero", "few values", "near", "outliers", "channel", "odd", "huge"])
+@pytest.mark.parametrize("G", [4, 9])                         # (three heads of forty pages are all scored in 64 bits: these are not)
+def test_selection_from_few_pages_by_their_scores(dtype, kind, G):
+    N, K = 40, 9
+    lo, hi = score_cache(kind, dtype, N)
+    table = torch.tensor([random.Random(N).sample(range(N), N)], dtype=torch.int32)
+    for power in (0, -60, -66, -72):
+        if power and kind != "plain":
+            continue
+        a, b = lo * 2.0 ** power, hi * 2.0 ** power
+        q = torch.randn(1, G, 64, generator=torch.Generator().manual_seed(1)).to(DT[dtype]) * 2.0 ** power
+        sel, n_sel = binding.page_select(q.cuda(), a.cuda(), b.cuda(), table.cuda(), i32([N * PAGE - 5]), K, N * PAGE - 5)
+        check_lists(sel, n_sel, ref.select(q, a, b, table, [N * PAGE - 5], K), K)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bad,query", [(-math.inf, 0.0), (-math.inf, -0.0), (math.nan, 0.0), (math.nan, 1.0), (math.inf, 1.0), (-math.inf, -1.0)])
+def test_selection_from_few_pages_with_an_infinity_or_nan(dtype, bad, query):
+    lo, hi = score_cache("plain", dtype, 40)
+    lo[7, :, 3] = bad
+    if bad == math.inf:
+        hi[7, :, 3] = bad
+    table = torch.arange(40, dtype=torch.int32)[None]
+    q = torch.randn(1, 5, 64, generator=torch.Generator().manual_seed(2)).to(DT[dtype])
+    q[0, :, 3] = q[0, :, 3].abs()
+    q[0, 1, 3] = query
+    sel, n_sel = binding.page_select(q.cuda(), lo.cuda(), hi.cuda(), table.cuda(), i32([640]), 9, 640)
+    check_lists(sel, n_sel, ref.select(q, lo, hi, table, [640], 9), 9)
 
 
 # ---------------------------------------------------------------------------------------------- attention
@@ -154,3 +187,35 @@ def test_a_plan_changes_the_lengths_of_those_that_get_tokens(rows):
     plan = binding.pages_plan(i32([0, 0, 0, 1, 1, 1]), lens, table, free, n_free, rows)
     assert plan.granted.tolist() == [0, 0, 0, 1, 1, 0] and plan.slot.tolist() == [10 * 16 + 7, 3 * 16, -1] + [-1] * (rows - 3)
     assert lens.tolist() == [-5, 1000, 20, 8, 1, 1000] and n_free.tolist() == [2]
+
+
+# ---------------------------------------------------------------------------------------------- append
+
+
+@pytest.mark.parametrize("dtype,T,Hk,D", [("bf16", 5003, 8, 64), ("bf16", 10007, 8, 64), ("fp32", 6001, 8, 64), ("bf16", 6001, 8, 128), ("fp32", 3001, 8, 128)])
+def test_append_in_windows_of_up_to_a_page(dtype, T, Hk, D):
+    """Rows of the list that a group of threads looks through at a time: as many as let all groups run at once, 9 in the first case, a page in the others."""
+    lanes = D * DT[dtype].itemsize // 16
+    block = min(PAGE, -(-2 * T * Hk * lanes // (148 * 512)))
+    assert block == (9 if T == 5003 else PAGE)
+    rng = random.Random(T)
+    n_pages = T // 4
+    pages, slots = rng.sample(range(n_pages), n_pages), []
+    while len(slots) < T:
+        kind = rng.random()
+        if kind < 0.15:
+            slots += [rng.choice([-1, -9, n_pages * PAGE, 2 ** 31 - 1])] * rng.choice([1, 1, 2, 5])
+            continue
+        page, start = pages.pop(), rng.choice([0, 0, rng.randrange(PAGE)])
+        n = rng.choice([1, PAGE - start, rng.randint(1, PAGE - start)])
+        slots += [page * PAGE + start + i for i in range(n)]
+    slots = slots[:T]
+    g = torch.Generator().manual_seed(T)
+    k, v = (torch.randn(T, Hk, D, generator=g).to(DT[dtype]) for _ in range(2))
+    cpu = [torch.randn(n_pages, Hk, PAGE, D, generator=g).to(DT[dtype]) for _ in range(2)]
+    cpu += [cpu[0].amin(2), cpu[0].amax(2)]
+    gpu = [t.cuda() for t in cpu]
+    binding.kv_append(k.cuda(), v.cuda(), i32(slots), *gpu)
+    ref.append(k, v, slots, *cpu)
+    for got, want in zip(gpu, cpu):
+        assert torch.equal(got.cpu(), want)
