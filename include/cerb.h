@@ -346,7 +346,8 @@ int cerb_pages_plan(const cerb_pages* state, const int32_t* n_new, int32_t rows,
 int cerb_pages_trim(const cerb_pages* state, const int32_t* keep, void* stream);
 
 /* Writes a step's keys and values into their slots.  With k_min and k_max (both or neither), element-wise minimum and maximum of the keys of a
- * page: of those of this call, and of what is there unless this call writes the page's slot 0 (which begins a page anew; NaN if a key is).
+ * page: of those of this call, and of what is there unless this call writes the page's slot 0 (which begins a page anew; NaN if a key is).  A page that a trim has cut keeps what its keys have left
+ * in them, those that are gone among them, until its slot 0 is written: a wider range, or a NaN, of which selection then makes a larger score, never a smaller one.
  * A page's tokens must be next to one another in the list, as cerb_pages_plan leaves them, and no slot come twice; otherwise what the pages
  * concerned hold is undefined. */
 typedef struct cerb_kv_append_args {

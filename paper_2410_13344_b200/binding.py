@@ -488,7 +488,8 @@ def gemm(X: torch.Tensor, W: torch.Tensor, scratch: Optional[torch.Tensor] = Non
     return out
 
 
-# ---- paged-cache operators of a serving loop (see the section on them in cerb.h); arguments are checked and outputs made in csrc/paged_binding.cpp
+# ---- paged-cache operators of a serving loop (see the section on them in cerb.h); arguments are checked and outputs made in csrc/paged_binding.cpp.
+# The tensors that a call returns are parts of one allocation: it is held as long as one of them is, saving one saves them all, and none may be resized.
 
 
 class PagePlan(NamedTuple):

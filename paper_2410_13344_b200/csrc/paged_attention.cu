@@ -11,7 +11,7 @@
 //   - a cluster per unit: the warps of a CTA in shared memory, its CTAs in each other's;
 //   - shares, long caches: all units' pages one after another in equal parts, one per CTA of a single wave; units that were cut are joined by a second kernel.
 // 64 sequences of up to 8192 tokens (64 heads on 8, heads of 128, 1257 MB) 187 us and 4 for the join: 6.7 TB/s in the main kernel, the rate of a copy; CTAs of equal shares
-// end between 172 and 187.  One sequence of 1000 tokens (32 heads on 8) 5.0 us a pass: 2.0 to the first keys' arrival, 0.4 for their products, the rest the meeting and the launch.
+// end between 172 and 187.  One sequence of 1000 tokens (32 heads on 8) 5.3 us a pass: 2.0 to the first keys' arrival, 0.4 for their products, the rest the meeting and the launch.
 #include <math.h>
 #include <string.h>
 
@@ -166,7 +166,8 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
 // interleaved into fragments by byte permutes.  S^T's sums become P^T's fragments by 8 x 8 transpositions of 16-bit elements.
 // P enters the second product as two bf16 terms, itself rounded and what that leaves, as in tree attention: a weight is off by at most 2^-16 of itself, and the sum l is that of the unrounded
 // ones; scores, maxima, sums and outputs are fp32.  (With one term a weight is off by up to 2^-8.  The second costs, us with one / two: 64 sequences of up to 8192 tokens 193.8 / 194.1, one of 1000
-// 5.6 / 5.7, 128 of 2000 with heads of 64 55.4 / 56.4, 16 of 4096 with 16 heads to a unit 26.9 / 27.4, 24 selections of 128 pages 65.6 / 65.9 with the selection.)
+// 5.6 / 5.7, 128 of 2000 with heads of 64 55.4 / 56.4, 16 of 4096 with 16 heads to a unit 26.9 / 27.4, 16 of 32768 with 16 / 64 heads on one KV head 54.7 / 56.1
+// and 154.5 / 161.6, 24 selections of 128 pages 65.6 / 65.9 with the selection.  The figures below that compare forms were taken with one.)
 // A warp takes KP pages at a time, 8 KB of keys and values, and has the next AHEAD times as many on their way.
 template <int DH, int NT, int AHEAD>
 __device__ __forceinline__ void attend_bf16(const PagedParams& p, const Piece& c, Sums<DH, 8 * NT>& sums) {
@@ -474,7 +475,8 @@ __device__ __forceinline__ void attend_f32(const PagedParams& p, const Piece& c,
 // every 128), the queries come out of shared memory, four chains of sums to a key and head keep the roundings in a row at Dh / 32 + 5.  Their GH x 4 sums meet by
 // halving, so that a lane has GH / 2 scores of one head.  Weights go through shared memory, two heads a pair; outputs: four columns to a lane
 // (heads of 64: every other key to each half of the warp).
-// 16 sequences of 8192 tokens, 8 heads of 128 on each of 8, 1074 MB: 170 us, 6.3 TB/s; 100 of 1600, 8 heads of 64, 655 MB: 120, 5.5 TB/s; the same with 16 heads, which takes two units: 185.
+// 16 sequences of 8192 tokens, 8 heads of 128 on each of 8, 1074 MB: 170 us, 6.3 TB/s; 100 of 1600, 8 heads of 64, 655 MB: 120, 5.5 TB/s; 16 heads, two units, each of which reads
+// the keys and values: 100 of 1600 220, 100 of 1280 185.
 // (With the lanes' way of the other fp32 form, 62 shuffles and 64 broadcasts for 8 keys of 8 heads: 216, 210, 326.  With a quarter of a key to a lane and weights twice in shared memory, the data
 // pipe of shared memory and L1 71 % busy: 191, 130, 201.  Four heads of 64 on each of 8, 16 x 9600 tokens: 127 -> 101 us, at the copy rate; four heads of 128: at the copy rate either way.)
 template <int DH, int GH>
