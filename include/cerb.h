@@ -366,7 +366,8 @@ int cerb_kv_append(const cerb_kv_append_args* args, void* stream);
  * out[b][h] = softmax over s of scale * q[b][h] . k[s], times v[s], with the KV head h / (n_heads / n_kv_heads); s are the
  * slots max(0, len[b] - window) .. len[b] - 1 (window 0: all), with a list those of them in the pages that it names: sel[b][kv head][i], i < n_sel[b],
  * logical pages in any order, entries outside the sequence count nothing, a page that comes twice counts twice.  No slots: out 0, lse -infinity.
- * lse = natural log of the softmax denominator.  Any n_heads divisible by n_kv_heads.  CERB_E_SHAPE: max_sel above 2^30. */
+ * lse = natural log of the softmax denominator.  Any n_heads divisible by n_kv_heads.  Scores are fp32, held times log2(e): |scale * q . k| from 2.3e38 on is infinite.
+ * CERB_E_SHAPE: max_sel above 2^30. */
 typedef struct cerb_paged_attn_args {
   int32_t dtype;                /* CERB_BF16 | CERB_F32 */
   int32_t B, n_heads, n_kv_heads, head_dim;     /* head_dim 64 or 128 */
